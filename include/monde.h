@@ -54,8 +54,8 @@ typedef enum {
     MONDE_ERR_BOUNDS = 7        /* diagnostics build only: an index read from memory was out of range */
 } monde_status;
 
-typedef enum { MONDE_F32 = 0, MONDE_BF16 = 1 } monde_dtype;
-typedef enum { MONDE_ACT_RELU = 0, MONDE_ACT_GELU_ERF = 1 } monde_act;
+typedef enum { MONDE_F32 = 0, MONDE_BF16 = 1, MONDE_E4M3 = 2 } monde_dtype;       /* MONDE_E4M3: monde_fp8.h only */
+typedef enum { MONDE_ACT_NONE = -1, MONDE_ACT_RELU = 0, MONDE_ACT_GELU_ERF = 1 } monde_act;   /* MONDE_ACT_NONE: monde_fp8.h only */
 
 typedef struct {
     int32_t T;              /* tokens (B*S) */
@@ -129,6 +129,7 @@ int monde_classify_top_h(const monde_problem* p, const int32_t* counts, double a
  *   x_perm[pos,:] = x[a / top_k,:]
  * in : x [T,d_model]; topk_idx [T,k]; offsets [E+1]
  * out: perm [A], inv_perm [A] int32; x_perm [A,d_model] (dtype)
+ * x and x_perm both NULL: perm and inv_perm alone (for a consumer that gathers rows by id itself).
  */
 int monde_permute(const monde_problem* p, const void* x, const int32_t* topk_idx,
                   const int32_t* offsets, int32_t* perm, int32_t* inv_perm, void* x_perm,

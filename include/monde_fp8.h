@@ -1,0 +1,106 @@
+/* monde_fp8.h -- the MoE FFN layer's operators in 8-bit floating point (e4m3 with fp32 scales).
+ *
+ * (The paper runs its layers in bf16 and has no counterpart.)  Cold experts and decode batches are bound by the bytes
+ * of the expert weights (paper Section 2.2), which 8-bit weights halve; hot experts get the tensor cores' doubled rate.
+ * A layer in this form is
+ *     monde_rmsnorm_quant          residual + norm, rows in 8 bits for the experts, in bf16 for the router
+ *     monde_route, monde_permute   as in monde.h (monde_permute with x = x_perm = NULL: ids alone)
+ *     monde_grouped_matmul_fp8     first expert matrix: gathers the 8-bit rows by id, bias, activation, 8-bit rows out
+ *     monde_grouped_matmul_fp8     second expert matrix
+ *     monde_combine                as in monde.h
+ * and a dense FFN layer the same with monde_matmul_fp8.  monde_quantize_fp8 lays out weights, and activations that come
+ * from elsewhere.  The conventions of monde.h hold: device pointers, row-major, caller-owned workspace, calls enqueue
+ * and return a monde_status, argument errors are found on the host before anything is launched.
+ *
+ * Representation.  An e4m3 value q (sign, 4 exponent bits, 3 mantissa bits, largest finite 448, no infinity) stands for
+ * q * scale, with one fp32 scale per block: 1 x 128 (a row's 128 consecutive columns) for activations, 128 x 128 for
+ * weights; blocks start at multiples of 128 and the last one of a row or column may be shorter.
+ *     amax  = largest magnitude in the block
+ *     scale = amax / 448, or 1 where amax < 2^-100 (such a block is stored as zeros)
+ *     q     = e4m3(v * (1 / scale))          round to nearest even
+ * A NaN makes its block's scale NaN, an infinity makes it infinite; either way the block reads back as NaN (or zero
+ * times infinity, which is NaN) and no other block is touched.
+ */
+#ifndef MONDE_FP8_H_
+#define MONDE_FP8_H_
+
+#include "monde.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* Residual addition, root-mean-square norm, quantisation; every output is optional.
+ *   v            = x + residual                                   (fp32; residual NULL: v = x)
+ *   residual_out = v                                              (rounded once to dtype)
+ *   u            = v * (1 / sqrt(mean over the row of v^2 + eps)) * gamma    (fp32, from the unrounded v; gamma NULL: 1)
+ *   y            = u                                              (rounded once to dtype)
+ *   q, scale     = u in 1 x 128 blocks                            (from the unrounded u)
+ * in : x [T,d], residual [T,d] or NULL, gamma [d] or NULL (dtype MONDE_F32 or MONDE_BF16)
+ * out: residual_out [T,d] (dtype) or NULL; y [T,d] (dtype) or NULL; q [T,d] e4m3 with scale [T, ceil(d/128)], both or
+ *      neither NULL.  residual_out and y may be x or residual themselves (with the same row stride).
+ * ld_*: distance between rows, in elements, >= d (>= ceil(d/128) for ld_scale).
+ * Limits: 1 <= d <= 32768.  T == 0 is valid.  Any alignment of rows; 16-byte aligned rows are the fast case.
+ */
+int monde_rmsnorm_quant(int32_t dtype, int32_t T, int32_t d, float eps, const void* x, int64_t ld_x,
+                        const void* residual, int64_t ld_residual, const void* gamma, void* residual_out,
+                        int64_t ld_residual_out, void* y, int64_t ld_y, void* q, int64_t ld_q, float* scale,
+                        int64_t ld_scale, void* stream);
+
+/* Quantisation of `batch` matrices [rows, cols] to e4m3 in blocks of block_rows x 128, block_rows 1 (activations) or
+ * 128 (weights; a block never spans two matrices of the batch).
+ * in : x [batch, rows, cols] (dtype MONDE_F32 or MONDE_BF16), rows ld_x elements apart, matrices rows * ld_x
+ * out: q [batch, rows, cols] e4m3, rows ld_q apart; scale [batch, ceil(rows/block_rows), ceil(cols/128)], rows ld_scale apart
+ */
+int monde_quantize_fp8(int32_t dtype, int32_t batch, int32_t rows, int32_t cols, int32_t block_rows, const void* x,
+                       int64_t ld_x, void* q, int64_t ld_q, float* scale, int64_t ld_scale, void* stream);
+
+/* Sizes of a product.  E = 1 for monde_matmul_fp8. */
+typedef struct {
+    int32_t rows;       /* rows of the output: T, or A = T*top_k positions of the expert-contiguous order */
+    int32_t N;          /* columns of the output = rows of a weight matrix */
+    int32_t K;          /* reduction length, a multiple of 16 */
+    int32_t E;          /* weight matrices */
+    int32_t src_rows;   /* rows of x; = rows unless row_ids is given */
+    int32_t row_div;    /* with row_ids: position r reads row row_ids[r] / row_div of x */
+    int32_t act;        /* MONDE_ACT_NONE, MONDE_ACT_RELU or MONDE_ACT_GELU_ERF */
+    int32_t out_dtype;  /* MONDE_BF16, MONDE_F32, or MONDE_E4M3 (out quantised in 1 x 128 blocks, out_scale written) */
+    int64_t ld_x;           /* distance between rows of x, bytes: >= K, a multiple of 16 */
+    int64_t ld_x_scale;     /* of x_scale, elements: >= ceil(K/128) */
+    int64_t ld_out;         /* of out, elements: >= N */
+    int64_t ld_out_scale;   /* of out_scale, elements: >= ceil(N/128) */
+} monde_matmul_problem;
+
+/* Bytes of scratch for a product of these sizes (at most MONDE_MATMUL_WS_MAX for any sizes); zero-filled once by the
+ * caller, with the rules of monde_workspace_bytes; also valid for monde_poll_device_status.  Products and layer calls
+ * on one stream may share a buffer that is large enough for each.  0 for an invalid problem. */
+#define MONDE_MATMUL_WS_MAX (48u << 20)
+size_t monde_matmul_workspace_bytes(const monde_matmul_problem* p);
+
+/* out[r,n] = act(bias[n] + sum over blocks b of x_scale[r,b] * w_scale[n/128,b] * sum_{k in b} x[r,k] * w[n,k])
+ * The inner sums are tensor-core products accumulated in fp32; scaling, the sum over blocks, bias and activation are in
+ * fp32; one rounding to out_dtype (MONDE_E4M3: the fp32 values are quantised as above).
+ * in : x [rows,K] e4m3, x_scale [rows, ceil(K/128)] fp32; w [N,K] e4m3, w_scale [ceil(N/128), ceil(K/128)] fp32;
+ *      bias [N] fp32 or NULL.  x and w 16-byte aligned.
+ * out: out [rows,N] (out_dtype); out_scale [rows, ceil(N/128)] fp32 with MONDE_E4M3, otherwise ignored
+ */
+int monde_matmul_fp8(const monde_matmul_problem* p, const void* x, const float* x_scale, const void* w,
+                     const float* w_scale, const float* bias, void* out, float* out_scale, void* ws, size_t ws_bytes,
+                     void* stream);
+
+/* The same product with one weight matrix per expert: rows offsets[e] .. offsets[e+1] of the output use w[e], w_scale[e],
+ * bias[e].  Reads offsets on the device; nothing comes back to the host.  Experts without rows are not read.  Rows past
+ * offsets[E] are not written.  A row id outside [0, src_rows * row_div) reads as a row of zeros.
+ * in : w [E,N,K], w_scale [E, ceil(N/128), ceil(K/128)], bias [E,N] or NULL; offsets [E+1] int32 ascending, as written by
+ *      monde_route; row_ids [rows] int32 or NULL (position r reads row r of x) - monde_permute's perm, with
+ *      row_div = top_k, reads every token's row where it lies, so no permuted copy is needed.
+ * Limits: E <= 256.
+ */
+int monde_grouped_matmul_fp8(const monde_matmul_problem* p, const void* x, const float* x_scale, const void* w,
+                             const float* w_scale, const float* bias, const int32_t* offsets, const int32_t* row_ids,
+                             void* out, float* out_scale, void* ws, size_t ws_bytes, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* MONDE_FP8_H_ */

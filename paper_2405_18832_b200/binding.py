@@ -1,4 +1,4 @@
-"""Thin ctypes binding of ``libmonde.so``: same names as ``include/monde.h``.
+"""Thin ctypes binding of ``libmonde.so``: same names as ``include/monde.h`` and ``include/monde_fp8.h``.
 
 Only argument marshalling happens here (device pointers of torch tensors, the
 problem struct, the current CUDA stream).  Every step of the layer runs in the
@@ -19,6 +19,8 @@ LIB_PATH = os.path.join(_HERE, "libmonde.so")
 SYMBOLS = ("monde_workspace_bytes", "monde_status_string", "monde_route", "monde_classify_top_h", "monde_permute",
            "monde_moe_ffn_fwd", "monde_moe_ffn_combine_fwd", "monde_moe_ffn_fwd_static_ws", "monde_combine", "monde_poll_device_status",
            "monde_kernel_launches", "monde_poll_static_ws_status",
+           "monde_rmsnorm_quant", "monde_quantize_fp8", "monde_matmul_workspace_bytes", "monde_matmul_fp8",
+           "monde_grouped_matmul_fp8",
            "monde_diag_set_ffn_cta_pairs", "monde_diag_set_trace", "monde_diag_set_wait_limit_ns",
            "monde_diag_set_hold_hidden_ready", "monde_diag_device_setups", "monde_diag_bounds_violations")
 
@@ -36,6 +38,11 @@ class MondeError(RuntimeError):
 class monde_problem(ctypes.Structure):
     _fields_ = [(n, ctypes.c_int32) for n in
                 ("T", "d_model", "d_ff", "E", "top_k", "hot_threshold", "renormalize", "dtype", "act")]
+
+
+class monde_matmul_problem(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "N", "K", "E", "src_rows", "row_div", "act", "out_dtype")] + \
+               [(n, ctypes.c_int64) for n in ("ld_x", "ld_x_scale", "ld_out", "ld_out_scale")]
 
 
 _lib = None
@@ -91,6 +98,18 @@ def lib() -> ctypes.CDLL:
         L.monde_diag_device_setups.argtypes = [ctypes.c_int]
         L.monde_diag_bounds_violations.restype = ctypes.c_int
         L.monde_diag_bounds_violations.argtypes = [ctypes.POINTER(ctypes.c_int32), ctypes.POINTER(ctypes.c_longlong)]
+        i32, i64, mp = ctypes.c_int32, ctypes.c_int64, ctypes.POINTER(monde_matmul_problem)
+        L.monde_rmsnorm_quant.restype = ctypes.c_int
+        L.monde_rmsnorm_quant.argtypes = [i32, i32, i32, ctypes.c_float, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, i64,
+                                          f32p, i64, vp]
+        L.monde_quantize_fp8.restype = ctypes.c_int
+        L.monde_quantize_fp8.argtypes = [i32, i32, i32, i32, i32, vp, i64, vp, i64, f32p, i64, vp]
+        L.monde_matmul_workspace_bytes.restype = ctypes.c_size_t
+        L.monde_matmul_workspace_bytes.argtypes = [mp]
+        L.monde_matmul_fp8.restype = ctypes.c_int
+        L.monde_matmul_fp8.argtypes = [mp, vp, f32p, vp, f32p, f32p, vp, f32p, vp, ctypes.c_size_t, vp]
+        L.monde_grouped_matmul_fp8.restype = ctypes.c_int
+        L.monde_grouped_matmul_fp8.argtypes = [mp, vp, f32p, vp, f32p, f32p, i32p, i32p, vp, f32p, vp, ctypes.c_size_t, vp]
         _lib = L
     return _lib
 
@@ -205,6 +224,129 @@ def monde_poll_device_status(ws, stream=None) -> None:
     st = lib().monde_poll_device_status(_ptr(ws), _stream(stream), ctypes.byref(site))
     if st != 0:
         raise MondeError(f"device status (site {site.value})", st)
+
+
+# ---- 8-bit floating point (include/monde_fp8.h) -------------------------------------------------------------------
+
+FP8_BLOCK = 128
+MATMUL_WS_MAX = 48 << 20
+_TORCH_DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float8_e4m3fn: 2}
+_MATMUL_ACT = {"none": -1, "relu": 0, "gelu": 1}
+
+
+def _mat(name, t, rows, cols, dtype):
+    """Checks a [rows, cols] CUDA matrix with contiguous rows; returns its address and the distance between rows."""
+    if t.dtype is not dtype or t.shape != (rows, cols) or not t.is_cuda:
+        raise ValueError(f"{name}: expected a CUDA tensor [{rows}, {cols}] of {dtype}, got {t.device} {tuple(t.shape)} {t.dtype}")
+    ld, one = t.stride()
+    if one != 1 and cols > 1:
+        raise ValueError(f"{name}: rows must be contiguous")
+    return t.data_ptr(), ld if rows > 1 else cols
+
+
+def _dense(name, t, shape, dtype):
+    if t.dtype is not dtype or t.shape != shape or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name}: expected a contiguous CUDA tensor {tuple(shape)} of {dtype}, "
+                         f"got {t.device} {tuple(t.shape)} {t.dtype}")
+    return t.data_ptr()
+
+
+def _raw_stream(stream):
+    return torch.cuda.current_stream().cuda_stream if stream is None else stream.cuda_stream
+
+
+def monde_rmsnorm_quant(x, residual, gamma, eps, residual_out, y, q, q_scale, stream=None) -> None:
+    """v = x + residual; residual_out = v; u = v / sqrt(mean v^2 + eps) * gamma; y = u; q, q_scale = u as e4m3 with a
+    scale per 1 x 128 block.  x [T, d] float32 or bfloat16; residual, gamma and each output may be None."""
+    T, d = x.shape
+    dt = x.dtype
+    px, lx = _mat("x", x, T, d, dt)
+    pr, lr = (0, 0) if residual is None else _mat("residual", residual, T, d, dt)
+    pg = 0 if gamma is None else _dense("gamma", gamma, (d,), dt)
+    po, lo = (0, 0) if residual_out is None else _mat("residual_out", residual_out, T, d, dt)
+    py, ly = (0, 0) if y is None else _mat("y", y, T, d, dt)
+    pq, lq = (0, 0) if q is None else _mat("q", q, T, d, torch.float8_e4m3fn)
+    ps, ls = (0, 0) if q_scale is None else _mat("q_scale", q_scale, T, -(-d // FP8_BLOCK), torch.float32)
+    st = lib().monde_rmsnorm_quant(_TORCH_DTYPE.get(dt, -1), T, d, eps, px, lx, pr, lr, pg, po, lo, py, ly, pq, lq, ps,
+                                   ls, _raw_stream(stream))
+    if st != 0:
+        raise MondeError("monde_rmsnorm_quant", st)
+
+
+def monde_quantize_fp8(x, q, q_scale, block_rows=1, stream=None) -> None:
+    """q, q_scale = x as e4m3 with a scale per block_rows x 128 block (1: activations, 128: weights).  x [rows, cols] or
+    [batch, rows, cols] (contiguous), float32 or bfloat16."""
+    dt = x.dtype
+    rows, cols = x.shape[-2:]
+    batch = 1
+    if x.dim() == 3:
+        batch = x.shape[0]
+        px, lx = _dense("x", x, x.shape, dt), cols
+        pq, lq = _dense("q", q, x.shape, torch.float8_e4m3fn), cols
+        ls = -(-cols // FP8_BLOCK)
+        ps = _dense("q_scale", q_scale, (batch, -(-rows // block_rows), ls), torch.float32)
+    else:
+        px, lx = _mat("x", x, rows, cols, dt)
+        pq, lq = _mat("q", q, rows, cols, torch.float8_e4m3fn)
+        ps, ls = _mat("q_scale", q_scale, -(-rows // block_rows), -(-cols // FP8_BLOCK), torch.float32)
+    st = lib().monde_quantize_fp8(_TORCH_DTYPE.get(dt, -1), batch, rows, cols, block_rows, px, lx, pq, lq, ps, ls,
+                                  _raw_stream(stream))
+    if st != 0:
+        raise MondeError("monde_quantize_fp8", st)
+
+
+def monde_matmul_workspace_bytes(rows, N, K, E=1, out_dtype=torch.bfloat16) -> int:
+    """Bytes of the zero-filled scratch buffer a product of these sizes needs (never more than MATMUL_WS_MAX)."""
+    cp = monde_matmul_problem(rows, N, K, E, rows, 1, -1, _TORCH_DTYPE[out_dtype], K, -(-K // FP8_BLOCK), N,
+                              -(-N // FP8_BLOCK))
+    return int(lib().monde_matmul_workspace_bytes(ctypes.byref(cp)))
+
+
+def _matmul(name, x, x_scale, w, w_scale, bias, offsets, row_ids, out, out_scale, ws, act, row_div, stream):
+    grouped = offsets is not None
+    rows, N = out.shape
+    src_rows, K = (rows, x.shape[1]) if row_ids is None else x.shape
+    E = w.shape[0] if grouped else 1
+    kb, nb = -(-K // FP8_BLOCK), -(-N // FP8_BLOCK)
+    e4m3, f32 = torch.float8_e4m3fn, torch.float32
+    px, lx = _mat("x", x, src_rows, K, e4m3)
+    pxs, lxs = _mat("x_scale", x_scale, src_rows, kb, f32)
+    lead = (E,) if grouped else ()
+    pw = _dense("w", w, lead + (N, K), e4m3)
+    pws = _dense("w_scale", w_scale, lead + (nb, kb), f32)
+    pb = 0 if bias is None else _dense("bias", bias, lead + (N,), f32)
+    dt = out.dtype
+    po, lo = _mat("out", out, rows, N, dt)
+    pos, los = (0, 0) if out_scale is None else _mat("out_scale", out_scale, rows, nb, f32)
+    cp = monde_matmul_problem(rows, N, K, E, src_rows, row_div, _MATMUL_ACT[act],
+                              _TORCH_DTYPE.get(dt, -1), lx, lxs, lo, los)
+    ref = ctypes.byref(cp)
+    pws_, nws = _dense("ws", ws, ws.shape, torch.uint8), ws.numel()
+    s = _raw_stream(stream)
+    if grouped:
+        poff = _dense("offsets", offsets, (E + 1,), torch.int32)
+        pid = 0 if row_ids is None else _dense("row_ids", row_ids, (rows,), torch.int32)
+        st = lib().monde_grouped_matmul_fp8(ref, px, pxs, pw, pws, pb, poff, pid, po, pos, pws_, nws, s)
+    else:
+        st = lib().monde_matmul_fp8(ref, px, pxs, pw, pws, pb, po, pos, pws_, nws, s)
+    if st != 0:
+        raise MondeError(name, st)
+
+
+def monde_matmul_fp8(x, x_scale, w, w_scale, bias, out, out_scale, ws, act="none", stream=None) -> None:
+    """out [rows, N] = act(x w^T + bias) of e4m3 operands x [rows, K] (scale per 1 x 128) and w [N, K] (scale per
+    128 x 128).  `out` bfloat16, float32, or float8_e4m3fn (quantised, scales to out_scale); act "none", "relu", "gelu"."""
+    _matmul("monde_matmul_fp8", x, x_scale, w, w_scale, bias, None, None, out, out_scale, ws, act, 1, stream)
+
+
+def monde_grouped_matmul_fp8(x, x_scale, w, w_scale, bias, offsets, row_ids, out, out_scale, ws, act="none", row_div=1,
+                             stream=None) -> None:
+    """monde_matmul_fp8 with one matrix per expert (w [E, N, K]): rows offsets[e] .. offsets[e+1] of `out` use expert e;
+    position r reads row r of x, or row row_ids[r] // row_div (monde_permute's perm with row_div = top_k)."""
+    if offsets is None:
+        raise ValueError("offsets: expected a CUDA tensor")
+    _matmul("monde_grouped_matmul_fp8", x, x_scale, w, w_scale, bias, offsets, row_ids, out, out_scale, ws, act, row_div,
+            stream)
 
 
 class LayerBuffers:

@@ -101,6 +101,8 @@ namespace {
 
 bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
+}  // namespace
+
 int check_arch() {
     int dev = 0, major = 0;
     if (cudaGetDevice(&dev) != cudaSuccess) return MONDE_ERR_CUDA;
@@ -108,6 +110,8 @@ int check_arch() {
         return MONDE_ERR_CUDA;
     return major == 10 ? MONDE_OK : MONDE_ERR_ARCH;
 }
+
+namespace {
 
 int check_ws(const monde_problem& p, const void* ws, size_t ws_bytes) {
     if (ws == nullptr || !aligned16(ws)) return MONDE_ERR_INVALID_ARG;
@@ -188,7 +192,7 @@ int monde_permute(const monde_problem* p, const void* x, const int32_t* topk_idx
     int st = check_problem(p);
     if (st != MONDE_OK) return st;
     if (p->T == 0) return MONDE_OK;
-    if (!x || !topk_idx || !offsets || !perm || !inv_perm || !x_perm) return MONDE_ERR_INVALID_ARG;
+    if (!topk_idx || !offsets || !perm || !inv_perm || (x == nullptr) != (x_perm == nullptr)) return MONDE_ERR_INVALID_ARG;
     if (!aligned16(x) || !aligned16(x_perm)) return MONDE_ERR_INVALID_ARG;
     if ((st = check_ws(*p, ws, ws_bytes)) != MONDE_OK) return st;
     if ((st = check_arch()) != MONDE_OK) return st;

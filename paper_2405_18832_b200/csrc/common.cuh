@@ -84,6 +84,7 @@ inline WsLayout ws_layout(const monde_problem& p) {
 
 // MONDE_OK when the problem is inside the stated limits.
 int check_problem(const monde_problem* p);
+int check_arch();      // MONDE_OK when the current device is compute capability 10.x
 // Pointer, alignment and architecture checks of monde_moe_ffn_fwd (everything but the workspace).
 int check_ffn_fwd_args(const void* x_perm, const void* W1, const void* b1, const void* W2, const void* b2,
                        const int32_t* counts, const int32_t* offsets, const uint8_t* cls, const int32_t* hot_ids,

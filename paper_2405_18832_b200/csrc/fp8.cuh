@@ -1,0 +1,86 @@
+// What the 8-bit floating-point kernels share: the block scale and its rounding, and 8-element row chunks.
+#pragma once
+
+#include <cuda_fp8.h>
+
+#include "../../include/monde_fp8.h"
+#include "common.cuh"
+
+namespace monde {
+
+constexpr int kFp8Block = 128;        // columns (and, for weights, rows) that share a scale
+constexpr float kE4m3Max = 448.0f;
+
+// Larger of two magnitudes; a NaN on either side stays (fmaxf would drop it, and a block with a NaN would read back finite).
+__device__ __forceinline__ float max_nan(float a, float b) {
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
+// amax / 448, or 1 for a block too small to divide by (2^-100: the reciprocal of the scale stays a normal number).
+// Both are kept in fp32: a scale rounded to fewer bits would add its error to all 128 values.
+__device__ __forceinline__ float block_scale(float amax) {
+    return amax < 7.8886090522101181e-31f ? 1.0f : __fdiv_rn(amax, kE4m3Max);
+}
+// Activations as in the bf16 layer, but a NaN stays one (relu by fmaxf would turn a poisoned block into zeros).
+__device__ __forceinline__ float apply_act_nan(float v, int act) {
+    if (act == MONDE_ACT_NONE) return v;
+    return act == MONDE_ACT_RELU ? max_nan(v, 0.0f) : apply_act(v, MONDE_ACT_GELU_ERF);
+}
+// Four values to e4m3, round to nearest even; the largest of a block lands on 448 (one rounding step of the product above
+// it at most, which rounds back), so nothing saturates.
+__device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d) {
+    const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(a, b), __NV_SATFINITE, __NV_E4M3);
+    const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(c, d), __NV_SATFINITE, __NV_E4M3);
+    return lo | (hi << 16);
+}
+
+// Eight consecutive elements of a row.  kVec: 16-byte accesses (base and row stride 16-byte multiples, d a multiple of 8);
+// otherwise element by element, elements at or past `n` read as zero and are not written.
+template <typename T, bool kVec>
+__device__ __forceinline__ void load8(const T* p, int n, float (&v)[8]) {
+    if constexpr (kVec) {
+        constexpr int V = Vec16<T>::N;
+#pragma unroll
+        for (int i = 0; i < 8 / V; ++i) {
+            float t[V];
+            Vec16<T>::load(p + i * V, t);
+#pragma unroll
+            for (int j = 0; j < V; ++j) v[i * V + j] = t[j];
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = j < n ? to_float(p[j]) : 0.0f;
+    }
+}
+template <typename T, bool kVec>
+__device__ __forceinline__ void store8(T* p, int n, const float (&v)[8]) {
+    if constexpr (kVec) {
+        constexpr int V = Vec16<T>::N;
+#pragma unroll
+        for (int i = 0; i < 8 / V; ++i) {
+            float t[V];
+#pragma unroll
+            for (int j = 0; j < V; ++j) t[j] = v[i * V + j];
+            Vec16<T>::store(p + i * V, t);
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < n) p[j] = from_float<T>(v[j]);
+    }
+}
+template <bool kVec>
+__device__ __forceinline__ void store8_e4m3(uint8_t* p, int n, const float (&v)[8], float inv) {
+    const uint32_t lo = pack_e4m3(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+    const uint32_t hi = pack_e4m3(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
+    if constexpr (kVec) {
+        *reinterpret_cast<uint2*>(p) = make_uint2(lo, hi);
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (j < n) p[j] = static_cast<uint8_t>((j < 4 ? lo : hi) >> (8 * (j & 3)));
+    }
+}
+
+}  // namespace monde

@@ -71,7 +71,7 @@ __global__ void __launch_bounds__(kThreads) permute_gather_kernel(
     // requested now, so that trip to memory overlaps the recount and the rank computation.
     constexpr int V = Vec16<T>::N;
     constexpr int kIter = 3;                         // vectors per lane and row in flight
-    const int vec_per_row = d / V;
+    const int vec_per_row = x_perm != nullptr ? d / V : 0;      // null: ids alone, no rows to copy
     const uint4* src[kRowsPerWarp];
     uint4 v[kIter][kRowsPerWarp];
 #pragma unroll
