@@ -199,7 +199,7 @@ __device__ __forceinline__ bool diag_in_range(bool ok, DiagRecord* rec, int site
 // each.  `per_device_once(key, fn)` runs `fn` once for the current device and the given key and
 // returns its (cached) result on every later call; keys are small integers owned by the callers.
 constexpr int kMaxDevices = 64;
-enum SetupKey { kSetupFfn = 0, kSetupRoute1, kSetupRoute2, kSetupRoute4, kSetupRoute8, kSetupKeys };
+enum SetupKey { kSetupFfn = 0, kSetupRoute1, kSetupRoute2, kSetupRoute4, kSetupRoute8, kSetupMatmulFp8, kSetupKeys };
 cudaError_t per_device_once(int key, cudaError_t (*fn)());
 int current_sm_count();        // multiprocessors of the current device (cached per device)
 

@@ -1,144 +1,584 @@
-// e4m3 matrix product with a scale per 128-block, dense and grouped by expert.
+// e4m3 matrix product with a scale per 128-block, dense and grouped by expert, on the tcgen05 tensor cores.
 //
 // out[r,n] = act(bias[n] + sum_b xs[r,b] ws[n/128,b] P_b[r,n]),  P_b[r,n] = sum_{k in block b} x[r,k] w[n,k].
+//
+// The scales of a block are general fp32 numbers, so the tensor core can only form P_b: each 128-wide K block is a fresh
+// accumulator in tensor memory (two buffers take turns), and two warpgroups add it, scaled, to the running sums in their
+// registers while the tensor core works on the next block.  Rows are the 128 lanes of tensor memory: a thread owns one
+// output row and 128 of its columns, i.e. exactly one weight-scale block, so the scale of a step is one number per thread,
+// and the 1 x 128 block of an e4m3 output is one thread's registers.
+//
+// A work unit is (expert, row tile, 256 columns, K range).  Tiles of one expert follow one another, rows fastest in groups,
+// so the tiles that run at the same time share weights and rows through L2.  When there are too few tiles for the SMs the
+// K range is split: every part leaves its fp32 sums in the workspace and the part that finishes last (a counter per tile)
+// adds them in the order of K, whoever it is, so results are bit-reproducible and nobody waits.
+#include <cuda.h>
+
 #include "fp8.cuh"
+#include "sm100.cuh"
 
 namespace monde {
 
 namespace {
 
+using namespace sm100;
+
 struct MatmulParams {
     int rows, N, K, E, src_rows, row_div, act, out_dtype;
-    int64_t ld_x, ld_x_scale, ld_out, ld_out_scale;
-    const uint8_t* x;
+    int64_t ld_x_scale, ld_out, ld_out_scale;
     const float* x_scale;
-    const uint8_t* w;
     const float* w_scale;
     const float* bias;
     const int32_t* offsets;     // null: one matrix, all rows
     const int32_t* row_ids;     // null: position r reads row r
     void* out;
     float* out_scale;
+    int out_vec;                // rows of `out` start on 16-byte boundaries
+    int32_t* status;            // {status, site}
+    int32_t* tickets;           // [tile][CTA of the pair][epilogue warp]: parts of a K-split tile that have finished (zero between calls)
+    float4* partials;           // [unit][CTA of the pair][column half][32][128 threads]
+    unsigned long long wait_ns;
 };
 
-constexpr int kTileM = 32, kTileN = 128, kSubK = 32;
-constexpr int kThreads = 256;
+// Boxes of the row operand: as many rows as a small tile needs (a box row that is not needed still costs its trip through
+// L2); with row ids one row, gathered four at a time.
+struct MatmulMaps {
+    CUtensorMap a[3];       // 128, 64, 32 rows
+    CUtensorMap w[2];       // the columns of a full and of a half tile
+};
 
-__device__ __forceinline__ float e4m3_to_float(uint8_t v) {
-    const __half_raw h = __nv_cvt_fp8_to_halfraw(v, __NV_E4M3);
-    return __half2float(__half(h));
+constexpr int kThreads = 384;          // warps 0-3: weight loads, MMA, row loads, spare; warps 4-11: two epilogue warpgroups
+constexpr int kTileN = 256;
+constexpr int kRowBytes = 128;         // K block: one swizzle row
+constexpr int kRowsPerCta = 128;
+constexpr int kABytes = kRowsPerCta * kRowBytes;
+constexpr int kMaxSplit = 16;
+constexpr int kMaxSplitUnits = 296;    // units of a K-split product: bounds the workspace
+constexpr size_t kUnitPartialBytes = size_t(kRowsPerCta) * kTileN * 4;
+constexpr int kStagePitch = 80;        // output staging: 64 bytes of a row, padded so that 8 lanes' 16-byte writes miss one another's banks
+constexpr int kStageWarpBytes = 32 * kStagePitch;
+constexpr int kRowGroup = 8;           // row tiles that go together through the columns
+
+template <bool kPair> struct Geometry {
+    static constexpr int kTileM = kPair ? 256 : 128;              // rows of a tile (a pair: 128 in each CTA)
+    static constexpr int kBBytes = (kPair ? 128 : 256) * kRowBytes;   // weight rows a CTA loads
+    static constexpr int kStageBytes = kABytes + kBBytes;
+    static constexpr int kStages = kPair ? 6 : 4;
+    static constexpr int kBars = 2 * kStages + 4;
+    static constexpr int kSmem = 1024 + kStages * kStageBytes + 8 * kStageWarpBytes + kBars * 8 + 64 + (2 * kMaxExperts + 4) * 4;
+};
+
+enum WaitSite { kSiteLoad = 21, kSiteMmaOperands = 22, kSiteMmaAcc = 23, kSiteEpilogue = 24 };
+
+__device__ __forceinline__ void give_up(int32_t* status, volatile int* abort_flag, int site) {
+    *abort_flag = 1;
+    if (atomicCAS(status, 0, MONDE_ERR_TIMEOUT) == 0) status[1] = site;
 }
 
-// One 32 x 128 tile at a time on the CUDA cores: every warp holds four rows, every lane four columns of each.
-__global__ void __launch_bounds__(kThreads) matmul_fp8_simt_kernel(const MatmulParams P) {
-    __shared__ float sx[kTileM][kSubK + 1], sw[kTileN][kSubK + 1];
-    __shared__ int src[kTileM];
-    __shared__ int prefix[kMaxExperts + 1], first[kMaxExperts + 1];
-    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+struct Tile {
+    int e, r0, rows;      // expert, first row, rows of the tile
+    int n0, cols;         // first column, columns
+    int tile, split;      // tile number, part of its K range
+    int kb0, kb1;
+};
+
+// The list of work units, the same in every CTA.
+struct Units {
+    const int* prefix;    // row tiles of the experts before e
+    const int* first;     // first row of expert e
+    int E, n_tiles, N, kb_all, splits, total, tile_m;
+    __device__ __forceinline__ Tile decode(int u) const {
+        Tile t;
+        t.tile = u / splits;
+        t.split = u - t.tile * splits;
+        int lo = 0, hi = E - 1;                       // largest e with prefix[e] * n_tiles <= tile (empty experts have no tiles)
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (prefix[mid] * n_tiles <= t.tile) lo = mid; else hi = mid - 1;
+        }
+        t.e = lo;
+        const int m_tiles = prefix[lo + 1] - prefix[lo];
+        int local = t.tile - prefix[lo] * n_tiles;
+        const int per_group = kRowGroup * n_tiles;
+        const int g = local / per_group;
+        local -= g * per_group;
+        const int in_group = min(kRowGroup, m_tiles - g * kRowGroup);
+        const int n = local / in_group;
+        const int m = g * kRowGroup + local - n * in_group;
+        t.r0 = first[lo] + m * tile_m;
+        t.rows = min(tile_m, first[lo + 1] - t.r0);
+        t.n0 = n * kTileN;
+        t.cols = min(kTileN, N - t.n0);
+        t.kb0 = static_cast<int>(static_cast<int64_t>(kb_all) * t.split / splits);
+        t.kb1 = static_cast<int>(static_cast<int64_t>(kb_all) * (t.split + 1) / splits);
+        return t;
+    }
+};
+
+// Parts of the K range: as many as shorten the longest CTA's work, counted in K blocks, where a split tile pays about
+// four K blocks for leaving and collecting its parts.
+__device__ __forceinline__ int choose_splits(int tiles, int workers, int kb_all) {
+    int best = 1, best_cost = (tiles + workers - 1) / workers * kb_all;
+    for (int s = 2; s <= kMaxSplit && s <= kb_all && tiles * s <= min(kMaxSplitUnits, 2 * workers); ++s) {
+        const int cost = (tiles * s + workers - 1) / workers * ((kb_all + s - 1) / s + 4);
+        if (cost < best_cost) { best = s; best_cost = cost; }
+    }
+    return best;
+}
+
+__device__ __forceinline__ int source_row(const MatmulParams& P, int r) {      // -1: no such row
+    if (P.row_ids == nullptr) return r;
+    const int id = P.row_ids[r];
+    const int s = id < 0 ? -1 : id / P.row_div;
+    return s < P.src_rows ? s : -1;
+}
+
+// 128 columns of 32 rows (a row per lane) to global memory, 64 bytes of each row at a time through shared memory, so that
+// stores are 64-byte runs of a row.  `word(i)`: 32-bit word i of this lane's row.
+template <int kEsize, typename F>
+__device__ __forceinline__ void store_rows(uint8_t* stage, uint8_t* out_row0, int64_t ld_bytes, int rows, int cols,
+                                           bool vec, int lane, F word) {
+    constexpr int kPasses = 128 * kEsize / 64;
+    const int bytes = cols * kEsize;
+#pragma unroll
+    for (int p = 0; p < kPasses; ++p) {
+        __syncwarp();
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            *reinterpret_cast<uint4*>(stage + lane * kStagePitch + c * 16) =
+                make_uint4(word(p * 16 + c * 4), word(p * 16 + c * 4 + 1), word(p * 16 + c * 4 + 2), word(p * 16 + c * 4 + 3));
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = i * 8 + (lane >> 2), at = p * 64 + (lane & 3) * 16;
+            if (row >= rows || at >= bytes) continue;
+            const uint8_t* src = stage + row * kStagePitch + (lane & 3) * 16;
+            uint8_t* dst = out_row0 + row * ld_bytes + at;
+            if (vec && at + 16 <= bytes) {
+                *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(src);
+            } else {
+                for (int j = 0; j < 16 && at + j < bytes; j += kEsize) {
+                    if constexpr (kEsize == 1) dst[j] = src[j];
+                    else if constexpr (kEsize == 2) *reinterpret_cast<uint16_t*>(dst + j) = *reinterpret_cast<const uint16_t*>(src + j);
+                    else *reinterpret_cast<uint32_t*>(dst + j) = *reinterpret_cast<const uint32_t*>(src + j);
+                }
+            }
+        }
+    }
+}
+
+template <bool kPair>
+__global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_constant__ MatmulMaps M, const MatmulParams P) {
+    using G = Geometry<kPair>;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+    uint8_t* staging = smem + G::kStages * G::kStageBytes;
+    uint64_t* bars = reinterpret_cast<uint64_t*>(staging + 8 * kStageWarpBytes);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + G::kBars);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    int* prefix = reinterpret_cast<int*>(tmem_slot + 16);
+    int* first = prefix + kMaxExperts + 2;
+    const uint32_t bar0 = smem_u32(bars);
+    const auto full = [&](int s) { return bar0 + 8u * s; };
+    const auto empty = [&](int s) { return bar0 + 8u * (G::kStages + s); };
+    const auto acc_full = [&](int b) { return bar0 + 8u * (2 * G::kStages + b); };
+    const auto acc_empty = [&](int b) { return bar0 + 8u * (2 * G::kStages + 2 + b); };
+
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const bool gather = P.row_ids != nullptr;
     pdl_launch_dependents();
+    if (tid == 0) {
+        *abort_flag = 0;
+        for (int s = 0; s < G::kStages; ++s) {
+            mbar_init(full(s), 1);      // the weight producer's expect_tx (of the leader CTA)
+            mbar_init(empty(s), 1);     // one commit
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(acc_full(b), 1);                    // one commit
+            mbar_init(acc_empty(b), kPair ? 16 : 8);      // the epilogue warps, of both CTAs
+        }
+        fence_barrier_init();
+        for (int i = 0; i < 3; ++i) prefetch_tensormap(&M.a[i]);
+        for (int i = 0; i < 2; ++i) prefetch_tensormap(&M.w[i]);
+    } else if (warp == 1) {
+        if (kPair) { tmem_alloc_pair(smem_u32(tmem_slot), 512); tmem_relinquish_pair(); }
+        else { tmem_alloc(smem_u32(tmem_slot), 512); tmem_relinquish(); }
+    }
     pdl_wait();
+
+    // ---- unit list: row tiles per expert, from the offsets (clamped: a bad list may not reach outside the output) ------
     for (int e = tid; e <= P.E; e += kThreads)
         first[e] = P.offsets != nullptr ? min(max(P.offsets[e], 0), P.rows) : (e == 0 ? 0 : P.rows);
     __syncthreads();
-    if (tid == 0) {
-        int run = 0;
-        for (int e = 0; e < P.E; ++e) {
-            prefix[e] = run;
-            run += max(0, first[e + 1] - first[e] + kTileM - 1) / kTileM;
+    if (warp == 0) {
+        int v[8], sum = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int e = lane * 8 + i;
+            v[i] = e < P.E ? (max(first[e + 1] - first[e], 0) + G::kTileM - 1) / G::kTileM : 0;
+            sum += v[i];
         }
-        prefix[P.E] = run;
+        int inc = sum;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int t = __shfl_up_sync(0xffffffffu, inc, o);
+            if (lane >= o) inc += t;
+        }
+        int run = inc - sum;
+        if (lane == 0) prefix[0] = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            run += v[i];
+            if (lane * 8 + i < P.E) prefix[lane * 8 + i + 1] = run;
+        }
     }
+    tc_fence_before_sync();
     __syncthreads();
-    const int nb = (P.N + kTileN - 1) / kTileN, kb = (P.K + kFp8Block - 1) / kFp8Block;
-    const int64_t total = static_cast<int64_t>(prefix[P.E]) * nb;
-    for (int64_t tile = blockIdx.x; tile < total; tile += gridDim.x) {
-        const int mt = static_cast<int>(tile / nb), nt = static_cast<int>(tile % nb);
-        int e = 0;
-        while (prefix[e + 1] <= mt) ++e;
-        const int r0 = first[e] + (mt - prefix[e]) * kTileM;
-        const int rows = min(kTileM, first[e + 1] - r0);
-        const int n0 = nt * kTileN;
-        __syncthreads();
-        if (tid < kTileM) {
-            int s = -1;
-            if (tid < rows) {
-                s = r0 + tid;
-                if (P.row_ids != nullptr) {
-                    const int id = P.row_ids[s];
-                    s = id < 0 ? -1 : id / P.row_div;
+    if (kPair) cluster_sync_all();
+    tc_fence_after_sync();
+    const uint32_t tmem_base = *tmem_slot;
+    const uint32_t rank = kPair ? cluster_ctarank() : 0u;
+    const uint32_t bar0_leader = kPair ? map_to_cta(bar0, 0) : bar0;
+    const int workers = kPair ? static_cast<int>(gridDim.x) / 2 : static_cast<int>(gridDim.x);
+    const int worker = kPair ? static_cast<int>(blockIdx.x) / 2 : static_cast<int>(blockIdx.x);
+    Units un;
+    un.prefix = prefix;
+    un.first = first;
+    un.E = P.E;
+    un.n_tiles = (P.N + kTileN - 1) / kTileN;
+    un.N = P.N;
+    un.kb_all = (P.K + kFp8Block - 1) / kFp8Block;
+    un.tile_m = G::kTileM;
+    const int tiles = prefix[P.E] * un.n_tiles;
+    un.splits = choose_splits(tiles, workers, un.kb_all);
+    un.total = tiles * un.splits;
+    const uint32_t stages_u32 = smem_u32(smem);
+
+    // Rows of the tile that CTA `r` of the pair holds, and the bytes its row loads bring.
+    const auto rows_of = [&](const Tile& t, uint32_t r) { return min(max(t.rows - static_cast<int>(r) * kRowsPerCta, 0), kRowsPerCta); };
+    const auto a_bytes_of = [&](int rows) {
+        if (gather) return (rows + 3) / 4 * 4 * kRowBytes;
+        return rows == 0 ? 0 : (rows <= 32 ? 32 : (rows <= 64 ? 64 : 128)) * kRowBytes;
+    };
+
+    if (warp < 4) {
+        regs_dec<40>();
+        if (warp == 0 && lane == 0) {
+            // ---- loads of weights and of contiguous rows ---------------------------------------------------------
+            const uint64_t pol_w = policy_evict_first(), pol_a = policy_evict_last();
+            int stage = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int u = worker; ok && u < un.total; u += workers) {
+                const Tile t = un.decode(u);
+                const int rows = rows_of(t, rank);
+                const bool half = t.cols <= kTileN / 2;
+                const CUtensorMap* mw = &M.w[half];
+                const int b_rows = (half ? kTileN / 2 : kTileN) / (kPair ? 2 : 1);
+                const CUtensorMap* ma = &M.a[rows <= 32 ? 2 : (rows <= 64 ? 1 : 0)];
+                const uint32_t bytes = a_bytes_of(rows_of(t, 0)) + (kPair ? a_bytes_of(rows_of(t, 1)) : 0) +
+                                       (kPair ? 2 : 1) * b_rows * kRowBytes;
+                const int w_row = t.e * P.N + t.n0 + static_cast<int>(rank) * b_rows;
+                const int a_row = t.r0 + static_cast<int>(rank) * kRowsPerCta;
+                for (int kb = t.kb0; kb < t.kb1; ++kb) {
+                    if (!mbar_wait(empty(stage), phase ^ 1, abort_flag, P.wait_ns)) {
+                        give_up(P.status, abort_flag, kSiteLoad);
+                        ok = false;
+                        break;
+                    }
+                    const uint32_t dst = stages_u32 + stage * G::kStageBytes;
+                    if (rank == 0) mbar_arrive_expect_tx(full(stage), bytes);
+                    if (kPair) {
+                        const uint32_t bar = bar0_leader + 8u * stage;
+                        tma_load_2d_pair(dst + kABytes, mw, bar, kb * kRowBytes, w_row, pol_w);
+                        if (!gather && rows > 0) tma_load_2d_pair(dst, ma, bar, kb * kRowBytes, a_row, pol_a);
+                    } else {
+                        tma_load_2d(dst + kABytes, mw, full(stage), kb * kRowBytes, w_row, pol_w);
+                        if (!gather) tma_load_2d(dst, ma, full(stage), kb * kRowBytes, a_row, pol_a);
+                    }
+                    if (++stage == G::kStages) { stage = 0; phase ^= 1; }
                 }
-                if (s >= P.src_rows) s = -1;
             }
-            src[tid] = s;
+        } else if (warp == 2 && gather) {
+            // ---- loads of rows picked by id: every lane four rows ------------------------------------------------
+            const uint64_t pol_a = policy_evict_last();
+            int stage = 0;
+            uint32_t phase = 0;
+            bool ok = true;
+            for (int u = worker; ok && u < un.total; u += workers) {
+                const Tile t = un.decode(u);
+                const int rows = rows_of(t, rank);
+                const int base = t.r0 + static_cast<int>(rank) * kRowsPerCta;
+                int4 src = make_int4(0, 0, 0, 0);       // a row that is not there reads row 0, and is not used
+                if (4 * lane < rows) {
+                    const auto pick = [&](int j) { return 4 * lane + j < rows ? max(source_row(P, base + 4 * lane + j), 0) : 0; };
+                    src = make_int4(pick(0), pick(1), pick(2), pick(3));
+                }
+                for (int kb = t.kb0; kb < t.kb1; ++kb) {
+                    // one lane waits for all (the outcome is shared), then every lane issues its own load
+                    int got = 1;
+                    if (lane == 0) got = mbar_wait(empty(stage), phase ^ 1, abort_flag, P.wait_ns);
+                    if (!__shfl_sync(0xffffffffu, got, 0)) {
+                        if (lane == 0) give_up(P.status, abort_flag, kSiteLoad);
+                        ok = false;
+                        break;
+                    }
+                    if (4 * lane < rows) {
+                        const uint32_t dst = stages_u32 + stage * G::kStageBytes + lane * 4 * kRowBytes;
+                        if (kPair) tma_gather4_pair(dst, &M.a[0], bar0_leader + 8u * stage, kb * kRowBytes, src, pol_a);
+                        else tma_gather4(dst, &M.a[0], full(stage), kb * kRowBytes, src, pol_a);
+                    }
+                    if (++stage == G::kStages) { stage = 0; phase ^= 1; }
+                }
+            }
+        } else if (warp == 1 && lane == 0 && rank == 0) {
+            // ---- MMA issue ---------------------------------------------------------------------------------------
+            int stage = 0, b = 0;
+            uint32_t phase = 0, acc_phase = 0;
+            bool ok = true;
+            for (int u = worker; ok && u < un.total; u += workers) {
+                const Tile t = un.decode(u);
+                const uint32_t idesc = idesc_e4m3(G::kTileM, t.cols <= kTileN / 2 ? kTileN / 2 : kTileN);
+                for (int kb = t.kb0; kb < t.kb1; ++kb) {
+                    if (!(kPair ? mbar_wait_cluster(acc_empty(b), acc_phase ^ 1, abort_flag, P.wait_ns)
+                                : mbar_wait(acc_empty(b), acc_phase ^ 1, abort_flag, P.wait_ns))) {
+                        give_up(P.status, abort_flag, kSiteMmaAcc);
+                        ok = false;
+                        break;
+                    }
+                    if (!(kPair ? mbar_wait_cluster(full(stage), phase, abort_flag, P.wait_ns)
+                                : mbar_wait(full(stage), phase, abort_flag, P.wait_ns))) {
+                        give_up(P.status, abort_flag, kSiteMmaOperands);
+                        ok = false;
+                        break;
+                    }
+                    tc_fence_after_sync();
+                    const uint64_t a = smem_desc_sw128(stages_u32 + stage * G::kStageBytes);
+                    const uint64_t w = smem_desc_sw128(stages_u32 + stage * G::kStageBytes + kABytes);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {        // 32 of the block's 128 columns each
+                        if (kPair) umma_f8_pair(tmem_base + b * kTileN, a + 2 * k, w + 2 * k, idesc, k != 0);
+                        else umma_f8(tmem_base + b * kTileN, a + 2 * k, w + 2 * k, idesc, k != 0);
+                    }
+                    if (kPair) { umma_commit_pair(empty(stage)); umma_commit_pair(acc_full(b)); }
+                    else { umma_commit(empty(stage)); umma_commit(acc_full(b)); }
+                    if (++stage == G::kStages) { stage = 0; phase ^= 1; }
+                    if (++b == 2) { b = 0; acc_phase ^= 1; }
+                }
+            }
         }
-        __syncthreads();
-        const uint8_t* w = P.w + static_cast<int64_t>(e) * P.N * P.K;
-        float acc[4][4] = {};
-        for (int b = 0; b < kb; ++b) {
-            float part[4][4] = {};
-            for (int k0 = b * kFp8Block; k0 < min(P.K, (b + 1) * kFp8Block); k0 += kSubK) {
-                for (int i = tid; i < kTileM * kSubK; i += kThreads) {
-                    const int r = i / kSubK, k = k0 + i % kSubK;
-                    sx[r][i % kSubK] = src[r] >= 0 && k < P.K ? e4m3_to_float(P.x[src[r] * P.ld_x + k]) : 0.0f;
+    } else {
+        // ---- epilogue: scale and add the blocks, then bias, activation, rounding and stores ----------------------
+        regs_inc<232>();
+        const int wg = (warp - 4) >> 2, quarter = warp & 3, wg_thread = tid - 128 - wg * 128;
+        uint8_t* stage_out = staging + (warp - 4) * kStageWarpBytes;
+        const uint32_t tmem_mine = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + wg * (kTileN / 2);
+        const uint32_t acc_empty_remote = kPair ? bar0_leader + 8u * (2 * G::kStages + 2) : 0u;
+        const int nb = (P.N + kFp8Block - 1) / kFp8Block;
+        int b = 0;
+        uint32_t acc_phase = 0;
+        bool ok = true;
+        for (int u = worker; ok && u < un.total; u += workers) {
+            const Tile t = un.decode(u);
+            const int row0 = t.r0 + static_cast<int>(rank) * kRowsPerCta + quarter * 32;       // of the warp
+            const int warp_rows = min(max(rows_of(t, rank) - quarter * 32, 0), 32);
+            const int n0 = t.n0 + wg * (kTileN / 2);
+            const int cols = min(max(P.N - n0, 0), kTileN / 2);
+            const bool active = warp_rows > 0 && cols > 0;         // the same for all lanes
+            const bool mine = active && lane < warp_rows;
+            const int src = mine ? source_row(P, row0 + lane) : -1;
+            const float* xs = P.x_scale + (src >= 0 ? src * P.ld_x_scale : 0);
+            const float* ws = P.w_scale + (static_cast<int64_t>(t.e) * nb + n0 / kFp8Block) * un.kb_all;
+            uint64_t acc[64];
+#pragma unroll
+            for (int i = 0; i < 64; ++i) acc[i] = 0;
+            float xs_next = 0.0f, ws_next = 0.0f;
+            if (active) { xs_next = xs[t.kb0]; ws_next = ws[t.kb0]; }
+            for (int kb = t.kb0; kb < t.kb1; ++kb) {
+                const float f = xs_next * ws_next;
+                if (active && kb + 1 < t.kb1) { xs_next = xs[kb + 1]; ws_next = ws[kb + 1]; }
+                if (!__all_sync(0xffffffffu, mbar_wait(acc_full(b), acc_phase, abort_flag, P.wait_ns))) {
+                    give_up(P.status, abort_flag, kSiteEpilogue);
+                    ok = false;
+                    break;
                 }
-                for (int i = tid; i < kTileN * kSubK; i += kThreads) {
-                    const int n = i / kSubK, k = k0 + i % kSubK;
-                    sw[n][i % kSubK] = n0 + n < P.N && k < P.K
-                        ? e4m3_to_float(w[static_cast<int64_t>(n0 + n) * P.K + k]) : 0.0f;
+                tc_fence_after_sync();
+                if (active) {
+                    const uint64_t f2 = pack2(__float_as_uint(f), __float_as_uint(f));
+                    uint32_t p0[32], p1[32];
+                    const uint32_t at = tmem_mine + b * kTileN;
+                    const auto add = [&](const uint32_t (&p)[32], int first_pair) {
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) acc[first_pair + i] = fma2(pack2(p[2 * i], p[2 * i + 1]), f2, acc[first_pair + i]);
+                    };
+                    tmem_ld_32(at, p0);
+                    tmem_ld_wait();
+                    tmem_ld_32(at + 32, p1);
+                    add(p0, 0);
+                    tmem_ld_wait();
+                    tmem_ld_32(at + 64, p0);
+                    add(p1, 16);
+                    tmem_ld_wait();
+                    tmem_ld_32(at + 96, p1);
+                    add(p0, 32);
+                    tmem_ld_wait();
+                    tc_fence_before_sync();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if (kPair) mbar_arrive_cluster(acc_empty_remote + 8u * b); else mbar_arrive(acc_empty(b));
+                    }
+                    add(p1, 48);
+                } else if (lane == 0) {
+                    if (kPair) mbar_arrive_cluster(acc_empty_remote + 8u * b); else mbar_arrive(acc_empty(b));
                 }
-                __syncthreads();
-                for (int k = 0; k < kSubK; ++k)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-#pragma unroll
-                        for (int j = 0; j < 4; ++j)
-                            part[i][j] = fmaf(sx[warp * 4 + i][k], sw[lane + 32 * j][k], part[i][j]);
-                __syncthreads();
+                if (++b == 2) { b = 0; acc_phase ^= 1; }
             }
-            const float ws = P.w_scale[(static_cast<int64_t>(e) * nb + nt) * kb + b];
+            if (!ok) break;
+
+            if (un.splits > 1) {
+                // leave the sums; the part that comes last collects all of them in the order of K.  Every warp keeps its own
+                // counter: nothing here waits for another warp.
+                if (!active) continue;
+                const size_t unit_float4 = kUnitPartialBytes / 16 * (kPair ? 2 : 1);
+                float4* mine_at = P.partials + static_cast<size_t>(u) * unit_float4 +
+                                  (static_cast<size_t>(rank) * 2 + wg) * 32 * 128 + wg_thread;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const int s = src[warp * 4 + i];
-                const float f = s >= 0 ? P.x_scale[s * P.ld_x_scale + b] * ws : 0.0f;
+                for (int i = 0; i < 32; ++i) {
+                    const float2 x = unpack2(acc[2 * i]), y = unpack2(acc[2 * i + 1]);
+                    __stcg(mine_at + i * 128, make_float4(x.x, x.y, y.x, y.y));
+                }
+                __threadfence();
+                __syncwarp();
+                int seen = 0;
+                if (lane == 0) {
+                    int32_t* ticket = P.tickets + (static_cast<int64_t>(t.tile) * 2 + rank) * 8 + (warp - 4);
+                    seen = atomicAdd(ticket, 1);
+                    if (seen == un.splits - 1) *ticket = 0;
+                    __threadfence();
+                }
+                if (__shfl_sync(0xffffffffu, seen, 0) != un.splits - 1) continue;
 #pragma unroll
-                for (int j = 0; j < 4; ++j) acc[i][j] = fmaf(f, part[i][j], acc[i][j]);
+                for (int i = 0; i < 64; ++i) acc[i] = 0;
+                const float4* part = mine_at - static_cast<size_t>(t.split) * unit_float4;
+                const uint64_t one2 = pack2(__float_as_uint(1.0f), __float_as_uint(1.0f));
+                for (int s = 0; s < un.splits; ++s) {
+#pragma unroll
+                    for (int i = 0; i < 32; ++i) {
+                        const float4 v = __ldcg(part + i * 128);
+                        acc[2 * i] = fma2(pack2(__float_as_uint(v.x), __float_as_uint(v.y)), one2, acc[2 * i]);
+                        acc[2 * i + 1] = fma2(pack2(__float_as_uint(v.z), __float_as_uint(v.w)), one2, acc[2 * i + 1]);
+                    }
+                    part += unit_float4;
+                }
             }
-        }
+            if (!active) continue;
+
+            float v[128];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int r = warp * 4 + i;
-            float amax = 0.0f;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int n = n0 + lane + 32 * j;
-                if (n >= P.N) { acc[i][j] = 0.0f; continue; }
-                if (P.bias != nullptr) acc[i][j] += P.bias[static_cast<int64_t>(e) * P.N + n];
-                acc[i][j] = apply_act_nan(acc[i][j], P.act);
-                amax = max_nan(amax, fabsf(acc[i][j]));
+            for (int i = 0; i < 64; ++i) {
+                const float2 x = unpack2(acc[i]);
+                v[2 * i] = x.x;
+                v[2 * i + 1] = x.y;
             }
-            float inv = 0.0f;
-            if (P.out_dtype == MONDE_E4M3) {
+            if (src < 0) {                       // no such row: zeros, whatever the gathered stand-in held
 #pragma unroll
-                for (int o = 16; o > 0; o >>= 1) amax = max_nan(amax, __shfl_xor_sync(0xffffffffu, amax, o));
-                const float s = block_scale(amax);
-                inv = __fdiv_rn(1.0f, s);
-                if (r < rows && lane == 0) P.out_scale[(r0 + r) * P.ld_out_scale + nt] = s;
+                for (int i = 0; i < 128; ++i) v[i] = 0.0f;
             }
-            if (r >= rows) continue;
+            if (P.bias != nullptr) {
+                const float* bias = P.bias + static_cast<int64_t>(t.e) * P.N + n0;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int n = n0 + lane + 32 * j;
-                if (n >= P.N) continue;
-                const int64_t at = (r0 + r) * P.ld_out + n;
-                if (P.out_dtype == MONDE_E4M3)
-                    static_cast<uint8_t*>(P.out)[at] = static_cast<uint8_t>(pack_e4m3(acc[i][j] * inv, 0.f, 0.f, 0.f));
-                else if (P.out_dtype == MONDE_BF16)
-                    static_cast<__nv_bfloat16*>(P.out)[at] = __float2bfloat16_rn(acc[i][j]);
-                else
-                    static_cast<float*>(P.out)[at] = acc[i][j];
+                for (int i = 0; i < 128; ++i)
+                    if (i < cols) v[i] += __ldg(bias + i);
+            }
+            if (P.act == MONDE_ACT_RELU) {
+#pragma unroll
+                for (int i = 0; i < 128; ++i) v[i] = max_nan(v[i], 0.0f);
+            } else if (P.act == MONDE_ACT_GELU_ERF) {
+#pragma unroll
+                for (int i = 0; i < 128; ++i) v[i] = apply_act(v[i], MONDE_ACT_GELU_ERF);
+            }
+            if (P.out_dtype == MONDE_BF16) {
+                store_rows<2>(stage_out, static_cast<uint8_t*>(P.out) + (row0 * P.ld_out + n0) * 2, P.ld_out * 2, warp_rows,
+                              cols, P.out_vec, lane, [&](int i) {
+                                  const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+                                  return *reinterpret_cast<const uint32_t*>(&h);
+                              });
+            } else if (P.out_dtype == MONDE_F32) {
+                store_rows<4>(stage_out, static_cast<uint8_t*>(P.out) + (row0 * P.ld_out + n0) * 4, P.ld_out * 4, warp_rows,
+                              cols, P.out_vec, lane, [&](int i) { return __float_as_uint(v[i]); });
+            } else {
+                float amax = 0.0f;
+                if (cols == kFp8Block) {
+#pragma unroll
+                    for (int i = 0; i < 128; ++i) amax = max_nan(amax, fabsf(v[i]));
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 128; ++i)
+                        if (i < cols) amax = max_nan(amax, fabsf(v[i]));
+                }
+                const float s = block_scale(amax), inv = __fdiv_rn(1.0f, s);
+                if (mine) P.out_scale[(row0 + lane) * P.ld_out_scale + n0 / kFp8Block] = s;
+                store_rows<1>(stage_out, static_cast<uint8_t*>(P.out) + row0 * P.ld_out + n0, P.ld_out, warp_rows, cols,
+                              P.out_vec, lane, [&](int i) {
+                                  return pack_e4m3(v[4 * i] * inv, v[4 * i + 1] * inv, v[4 * i + 2] * inv, v[4 * i + 3] * inv);
+                              });
             }
         }
     }
+
+    // ---- teardown --------------------------------------------------------------------------------------------------
+    __syncwarp();
+    if (*abort_flag != 0) {      // a wait gave up: copies and MMAs in flight get the time they need to land before the CTA leaves
+        const uint64_t t0 = global_timer_ns();
+        while (global_timer_ns() - t0 < 200000ull) { }
+    }
+    tc_fence_before_sync();
+    __syncthreads();
+    if (kPair) cluster_sync_all();
+    if (warp == 1) {
+        tc_fence_after_sync();
+        if (kPair) tmem_dealloc_pair(tmem_base, 512); else tmem_dealloc(tmem_base, 512);
+    }
+}
+
+// ---- host side ---------------------------------------------------------------------------------------------------------
+
+using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                   CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+EncodeTiledFn encode_tiled_fn() {
+    static EncodeTiledFn fn = [] {
+        void* p = nullptr;
+        cudaDriverEntryPointQueryResult q;
+        if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &p, cudaEnableDefault, &q) != cudaSuccess ||
+            q != cudaDriverEntryPointSuccess)
+            p = nullptr;
+        return reinterpret_cast<EncodeTiledFn>(p);
+    }();
+    return fn;
+}
+
+// Row-major bytes [rows, cols], rows `ld` apart, in boxes of box_rows x 128 with the 128-byte swizzle; columns past the end
+// read as zeros (e4m3 zero), which is what the last, shorter K block needs.
+bool make_map(CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint64_t ld, uint32_t box_rows) {
+    EncodeTiledFn fn = encode_tiled_fn();
+    if (fn == nullptr) return false;
+    const cuuint64_t dims[2] = {cols, rows};
+    const cuuint64_t strides[1] = {ld};
+    const cuuint32_t box[2] = {kRowBytes, box_rows};
+    const cuuint32_t estr[2] = {1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT8, 2, const_cast<void*>(base), dims, strides, box, estr,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+cudaError_t matmul_kernel_attributes() {
+    cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(matmul_fp8_kernel<false>),
+                                         cudaFuncAttributeMaxDynamicSharedMemorySize, Geometry<false>::kSmem);
+    if (e != cudaSuccess) return e;
+    return cudaFuncSetAttribute(reinterpret_cast<const void*>(matmul_fp8_kernel<true>),
+                                cudaFuncAttributeMaxDynamicSharedMemorySize, Geometry<true>::kSmem);
 }
 
 int check_matmul(const monde_matmul_problem* p) {
@@ -158,7 +598,10 @@ int check_matmul(const monde_matmul_problem* p) {
 
 bool aligned(const void* p, unsigned m) { return (reinterpret_cast<uintptr_t>(p) & (m - 1)) == 0; }
 
-size_t matmul_ws_bytes(const monde_matmul_problem&) { return WsLayout::kHidden; }
+// Header as in the layer's workspace, then the parts of K-split tiles.
+size_t matmul_ws_bytes(const monde_matmul_problem&) { return WsLayout::kHidden + kMaxSplitUnits * kUnitPartialBytes; }
+static_assert(WsLayout::kHidden + kMaxSplitUnits * kUnitPartialBytes <= MONDE_MATMUL_WS_MAX, "workspace bound");
+static_assert(kMaxSplitUnits * 16 * 4 <= WsLayout::kPartDoneBytes, "tickets fit the header");
 
 int matmul(const monde_matmul_problem* p, const void* x, const float* x_scale, const void* w, const float* w_scale,
            const float* bias, bool grouped, const int32_t* offsets, const int32_t* row_ids, void* out, float* out_scale,
@@ -178,22 +621,41 @@ int matmul(const monde_matmul_problem* p, const void* x, const float* x_scale, c
     if (ws == nullptr || !aligned(ws, 16)) return MONDE_ERR_INVALID_ARG;
     if (ws_bytes < matmul_ws_bytes(*p)) return MONDE_ERR_WORKSPACE;
     if ((st = check_arch()) != MONDE_OK) return st;
+    if (per_device_once(kSetupMatmulFp8, matmul_kernel_attributes) != cudaSuccess) return MONDE_ERR_CUDA;
+    const DiagState diag = diag_state();
+    const bool pair = diag.ffn_pair > 0;
+    const int64_t row_tiles = p->rows / 128 + static_cast<int64_t>(p->E) + 1, col_tiles = (p->N + kTileN - 1) / kTileN;
+    if (row_tiles * col_tiles > (1 << 28) || static_cast<int64_t>(p->E) * p->N > 0x7fffff00 || p->K > 0x7fffff00 - 256)
+        return MONDE_ERR_UNSUPPORTED;
+    char* base = static_cast<char*>(ws);
     MatmulParams P;
     P.rows = p->rows; P.N = p->N; P.K = p->K; P.E = p->E;
     P.src_rows = p->src_rows; P.row_div = p->row_div; P.act = p->act; P.out_dtype = p->out_dtype;
-    P.ld_x = p->ld_x; P.ld_x_scale = p->ld_x_scale; P.ld_out = p->ld_out; P.ld_out_scale = p->ld_out_scale;
-    P.x = static_cast<const uint8_t*>(x);
+    P.ld_x_scale = p->ld_x_scale; P.ld_out = p->ld_out; P.ld_out_scale = p->ld_out_scale;
     P.x_scale = x_scale;
-    P.w = static_cast<const uint8_t*>(w);
     P.w_scale = w_scale;
     P.bias = bias;
     P.offsets = offsets;
     P.row_ids = row_ids;
     P.out = out;
     P.out_scale = out_scale;
-    if (launch_pdl(matmul_fp8_simt_kernel, dim3(current_sm_count() * 4), dim3(kThreads), 0,
-                   static_cast<cudaStream_t>(stream), P) != cudaSuccess)
-        return MONDE_ERR_CUDA;
+    P.out_vec = aligned(out, 16) && (p->ld_out * ob) % 16 == 0;
+    P.status = reinterpret_cast<int32_t*>(base + WsLayout::kStatus);
+    P.tickets = reinterpret_cast<int32_t*>(base + WsLayout::kPartDone);
+    P.partials = reinterpret_cast<float4*>(base + WsLayout::kHidden);
+    P.wait_ns = diag.wait_limit_ns;
+    MatmulMaps M;
+    for (int i = 0; i < 3; ++i) {
+        if (!make_map(&M.a[i], x, p->src_rows, p->K, p->ld_x, row_ids != nullptr ? 1 : kRowsPerCta >> i)) return MONDE_ERR_CUDA;
+        if (i < 2 && !make_map(&M.w[i], w, static_cast<uint64_t>(p->E) * p->N, p->K, p->K, (pair ? 128 : 256) >> i))
+            return MONDE_ERR_CUDA;
+    }
+    const int sms = current_sm_count();
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const cudaError_t err = pair
+        ? launch_pdl_cluster(matmul_fp8_kernel<true>, dim3(sms & ~1), dim3(kThreads), Geometry<true>::kSmem, 2, s, M, P)
+        : launch_pdl(matmul_fp8_kernel<false>, dim3(sms), dim3(kThreads), Geometry<false>::kSmem, s, M, P);
+    if (err != cudaSuccess) return MONDE_ERR_CUDA;
     return launched();
 }
 
