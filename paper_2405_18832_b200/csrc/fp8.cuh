@@ -10,6 +10,7 @@ namespace monde {
 
 constexpr int kFp8Block = 128;        // columns (and, for weights, rows) that share a scale
 constexpr float kE4m3Max = 448.0f;
+constexpr float kTinyAmax = 7.8886090522101181e-31f;      // 2^-100: blocks below it are stored as zeros
 
 // Larger of two magnitudes; a NaN on either side stays (fmaxf would drop it, and a block with a NaN would read back finite).
 __device__ __forceinline__ float max_nan(float a, float b) {
@@ -17,10 +18,10 @@ __device__ __forceinline__ float max_nan(float a, float b) {
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
-// amax / 448, or 1 for a block too small to divide by (2^-100: the reciprocal of the scale stays a normal number).
+// amax / 448, or 1 for a block too small to divide by (the reciprocal of any other scale is a normal number).
 // Both are kept in fp32: a scale rounded to fewer bits would add its error to all 128 values.
 __device__ __forceinline__ float block_scale(float amax) {
-    return amax < 7.8886090522101181e-31f ? 1.0f : __fdiv_rn(amax, kE4m3Max);
+    return amax < kTinyAmax ? 1.0f : __fdiv_rn(amax, kE4m3Max);
 }
 // Activations as in the bf16 layer, but a NaN stays one (relu by fmaxf would turn a poisoned block into zeros).
 __device__ __forceinline__ float apply_act_nan(float v, int act) {
@@ -35,24 +36,37 @@ __device__ __forceinline__ uint32_t pack_e4m3(float a, float b, float c, float d
     return lo | (hi << 16);
 }
 
-// Eight consecutive elements of a row.  kVec: 16-byte accesses (base and row stride 16-byte multiples, d a multiple of 8);
-// otherwise element by element, elements at or past `n` read as zero and are not written.
-template <typename T, bool kVec>
-__device__ __forceinline__ void load8(const T* p, int n, float (&v)[8]) {
-    if constexpr (kVec) {
-        constexpr int V = Vec16<T>::N;
+// Eight consecutive elements of a row, as they lie in memory: loads are issued without touching their results, so that a
+// thread's loads from several arrays are in flight together.  kVec: 16-byte accesses (base and row stride 16-byte multiples,
+// d a multiple of 8); otherwise element by element.  Elements at or past `n` read as zero and are not written.
+template <typename T> struct alignas(16) Raw8 {
+    T v[8];
+    template <bool kVec> __device__ __forceinline__ void load(const T* p, int n) {
+        if constexpr (kVec) {
+            constexpr int V = 8 * sizeof(T) / 16;
 #pragma unroll
-        for (int i = 0; i < 8 / V; ++i) {
-            float t[V];
-            Vec16<T>::load(p + i * V, t);
+            for (int i = 0; i < V; ++i)
+                reinterpret_cast<uint4*>(v)[i] = n > 0 ? reinterpret_cast<const uint4*>(p)[i] : make_uint4(0, 0, 0, 0);
+        } else {
 #pragma unroll
-            for (int j = 0; j < V; ++j) v[i * V + j] = t[j];
+            for (int j = 0; j < 8; ++j) v[j] = j < n ? p[j] : from_float<T>(0.0f);
         }
-    } else {
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = j < n ? to_float(p[j]) : 0.0f;
     }
-}
+    __device__ __forceinline__ float operator[](int j) const { return to_float(v[j]); }
+    __device__ __forceinline__ float amax() const {       // of the magnitudes; bf16 two at a time (exact in either type)
+        if constexpr (sizeof(T) == 2) {
+            const __nv_bfloat162* h = reinterpret_cast<const __nv_bfloat162*>(v);
+            const __nv_bfloat162 m = __hmax2_nan(__hmax2_nan(__habs2(h[0]), __habs2(h[1])),
+                                                 __hmax2_nan(__habs2(h[2]), __habs2(h[3])));
+            return max_nan(__low2float(m), __high2float(m));
+        } else {
+            float m = fabsf(v[0]);
+#pragma unroll
+            for (int j = 1; j < 8; ++j) m = max_nan(m, fabsf(v[j]));
+            return m;
+        }
+    }
+};
 template <typename T, bool kVec>
 __device__ __forceinline__ void store8(T* p, int n, const float (&v)[8]) {
     if constexpr (kVec) {
