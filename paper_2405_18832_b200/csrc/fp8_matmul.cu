@@ -33,6 +33,7 @@ struct MatmulParams {
     const int32_t* row_ids;     // null: position r reads row r
     void* out;
     float* out_scale;
+    int xs_vec;                 // rows of x_scale: 16-byte boundaries and whole groups of four
     int out_vec;                // rows of `out` start on 16-byte boundaries
     int32_t* status;            // {status, site}
     int32_t* tickets;           // [tile][CTA of the pair][epilogue warp]: parts of a K-split tile that have finished (zero between calls)
@@ -49,6 +50,10 @@ struct MatmulMaps {
 
 constexpr int kThreads = 384;          // warps 0-3: weight loads, MMA, row loads, spare; warps 4-11: two epilogue warpgroups
 constexpr int kTileN = 256;
+// Hardware barriers.  Full: an accumulator is finished (the polling warp and one epilogue warpgroup, [buffer][warpgroup]).
+// Empty: it has been read (both warpgroups and the MMA warp).  With every epilogue warp polling the mbarriers themselves,
+// each of these hand-overs took over a thousand cycles, three times the multiplication.
+constexpr int kBarFull = 1, kFullThreads = 128 + 32, kBarEmpty = 5, kEmptyThreads = 256 + 32;
 constexpr int kRowBytes = 128;         // K block: one swizzle row
 constexpr int kRowsPerCta = 128;
 constexpr int kABytes = kRowsPerCta * kRowBytes;
@@ -59,14 +64,6 @@ constexpr int kStagePitch = 80;        // output staging: 64 bytes of a row, pad
 constexpr int kStageWarpBytes = 32 * kStagePitch;
 constexpr int kRowGroup = 8;           // row tiles that go together through the columns
 
-template <bool kPair> struct Geometry {
-    static constexpr int kTileM = kPair ? 256 : 128;              // rows of a tile (a pair: 128 in each CTA)
-    static constexpr int kBBytes = (kPair ? 128 : 256) * kRowBytes;   // weight rows a CTA loads
-    static constexpr int kStageBytes = kABytes + kBBytes;
-    static constexpr int kStages = kPair ? 6 : 4;
-    static constexpr int kBars = 2 * kStages + 4;
-    static constexpr int kSmem = 1024 + kStages * kStageBytes + 8 * kStageWarpBytes + kBars * 8 + 64 + (2 * kMaxExperts + 4) * 4;
-};
 
 enum WaitSite { kSiteLoad = 21, kSiteMmaOperands = 22, kSiteMmaAcc = 23, kSiteEpilogue = 24 };
 
@@ -82,12 +79,14 @@ struct Tile {
     int kb0, kb1;
 };
 
-// The list of work units, the same in every CTA.
+// The list of work units, the same in every CTA.  It stays in shared memory: a few registers more in every role made all of
+// them spill.
 struct Units {
-    const int* prefix;    // row tiles of the experts before e
-    const int* first;     // first row of expert e
-    int E, n_tiles, N, kb_all, splits, total, tile_m;
-    __device__ __forceinline__ Tile decode(int u) const {
+    int total, splits;              // units; parts per tile
+    int n_tiles, kb_all;            // 256-column tiles of a row tile; K blocks
+    int prefix[kMaxExperts + 1];    // row tiles of the experts before e
+    int first[kMaxExperts + 1];     // first row of expert e
+    __device__ __forceinline__ Tile decode(int u, int E, int N, int tile_m) const {
         Tile t;
         t.tile = u / splits;
         t.split = u - t.tile * splits;
@@ -109,10 +108,19 @@ struct Units {
         t.rows = min(tile_m, first[lo + 1] - t.r0);
         t.n0 = n * kTileN;
         t.cols = min(kTileN, N - t.n0);
-        t.kb0 = static_cast<int>(static_cast<int64_t>(kb_all) * t.split / splits);
-        t.kb1 = static_cast<int>(static_cast<int64_t>(kb_all) * (t.split + 1) / splits);
+        t.kb0 = static_cast<unsigned>(kb_all * t.split) / splits;          // (K < 2^31, at most 16 parts: no overflow)
+        t.kb1 = static_cast<unsigned>(kb_all * (t.split + 1)) / splits;
         return t;
     }
+};
+
+template <bool kPair> struct Geometry {
+    static constexpr int kTileM = kPair ? 256 : 128;              // rows of a tile (a pair: 128 in each CTA)
+    static constexpr int kBBytes = (kPair ? 128 : 256) * kRowBytes;   // weight rows a CTA loads
+    static constexpr int kStageBytes = kABytes + kBBytes;
+    static constexpr int kStages = kPair ? 6 : 4;
+    static constexpr int kBars = 2 * kStages + 4;
+    static constexpr int kSmem = 1024 + kStages * kStageBytes + 8 * kStageWarpBytes + kBars * 8 + 64 + static_cast<int>(sizeof(Units));
 };
 
 // Parts of the K range: as many as shorten the longest CTA's work, counted in K blocks, where a split tile pays about
@@ -176,13 +184,14 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
     uint64_t* bars = reinterpret_cast<uint64_t*>(staging + 8 * kStageWarpBytes);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + G::kBars);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    int* prefix = reinterpret_cast<int*>(tmem_slot + 16);
-    int* first = prefix + kMaxExperts + 2;
+    Units& un = *reinterpret_cast<Units*>(tmem_slot + 16);
+    int* const prefix = un.prefix;
+    int* const first = un.first;
     const uint32_t bar0 = smem_u32(bars);
     const auto full = [&](int s) { return bar0 + 8u * s; };
     const auto empty = [&](int s) { return bar0 + 8u * (G::kStages + s); };
     const auto acc_full = [&](int b) { return bar0 + 8u * (2 * G::kStages + b); };
-    const auto acc_empty = [&](int b) { return bar0 + 8u * (2 * G::kStages + 2 + b); };
+    const auto peer_empty = [&](int b) { return bar0 + 8u * (2 * G::kStages + 2 + b); };
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const bool gather = P.row_ids != nullptr;
@@ -195,7 +204,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(acc_full(b), 1);                    // one commit
-            mbar_init(acc_empty(b), kPair ? 16 : 8);      // the epilogue warps, of both CTAs
+            mbar_init(peer_empty(b), 1);                  // the other CTA of a pair has read its half
         }
         fence_barrier_init();
         for (int i = 0; i < 3; ++i) prefetch_tensormap(&M.a[i]);
@@ -232,6 +241,18 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
             if (lane * 8 + i < P.E) prefix[lane * 8 + i + 1] = run;
         }
     }
+    const int workers = kPair ? static_cast<int>(gridDim.x) / 2 : static_cast<int>(gridDim.x);
+    const int worker = kPair ? static_cast<int>(blockIdx.x) / 2 : static_cast<int>(blockIdx.x);
+    if (warp == 0) {
+        __syncwarp();
+        if (lane == 0) {
+            un.n_tiles = (P.N + kTileN - 1) / kTileN;
+            un.kb_all = (P.K + kFp8Block - 1) / kFp8Block;
+            const int tiles = prefix[P.E] * un.n_tiles;
+            un.splits = choose_splits(tiles, workers, un.kb_all);
+            un.total = tiles * un.splits;
+        }
+    }
     tc_fence_before_sync();
     __syncthreads();
     if (kPair) cluster_sync_all();
@@ -239,19 +260,6 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
     const uint32_t tmem_base = *tmem_slot;
     const uint32_t rank = kPair ? cluster_ctarank() : 0u;
     const uint32_t bar0_leader = kPair ? map_to_cta(bar0, 0) : bar0;
-    const int workers = kPair ? static_cast<int>(gridDim.x) / 2 : static_cast<int>(gridDim.x);
-    const int worker = kPair ? static_cast<int>(blockIdx.x) / 2 : static_cast<int>(blockIdx.x);
-    Units un;
-    un.prefix = prefix;
-    un.first = first;
-    un.E = P.E;
-    un.n_tiles = (P.N + kTileN - 1) / kTileN;
-    un.N = P.N;
-    un.kb_all = (P.K + kFp8Block - 1) / kFp8Block;
-    un.tile_m = G::kTileM;
-    const int tiles = prefix[P.E] * un.n_tiles;
-    un.splits = choose_splits(tiles, workers, un.kb_all);
-    un.total = tiles * un.splits;
     const uint32_t stages_u32 = smem_u32(smem);
 
     // Rows of the tile that CTA `r` of the pair holds, and the bytes its row loads bring.
@@ -261,16 +269,24 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
         return rows == 0 ? 0 : (rows <= 32 ? 32 : (rows <= 64 ? 64 : 128)) * kRowBytes;
     };
 
+    // Whole warps wait, and one lane of them issues: a lane that loops alone while the others sit at the end of the branch
+    // took some 350 cycles more per turn.
+    const auto wait_all = [&](uint32_t bar, uint32_t parity, int site) {
+        if (__all_sync(0xffffffffu, mbar_wait(bar, parity, abort_flag, P.wait_ns))) return true;
+        if (lane == 0) give_up(P.status, abort_flag, site);
+        return false;
+    };
+
     if (warp < 4) {
         regs_dec<40>();
-        if (warp == 0 && lane == 0) {
+        if (warp == 0) {
             // ---- loads of weights and of contiguous rows ---------------------------------------------------------
             const uint64_t pol_w = policy_evict_first(), pol_a = policy_evict_last();
             int stage = 0;
             uint32_t phase = 0;
             bool ok = true;
             for (int u = worker; ok && u < un.total; u += workers) {
-                const Tile t = un.decode(u);
+                const Tile t = un.decode(u, P.E, P.N, G::kTileM);
                 const int rows = rows_of(t, rank);
                 const bool half = t.cols <= kTileN / 2;
                 const CUtensorMap* mw = &M.w[half];
@@ -281,21 +297,20 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
                 const int w_row = t.e * P.N + t.n0 + static_cast<int>(rank) * b_rows;
                 const int a_row = t.r0 + static_cast<int>(rank) * kRowsPerCta;
                 for (int kb = t.kb0; kb < t.kb1; ++kb) {
-                    if (!mbar_wait(empty(stage), phase ^ 1, abort_flag, P.wait_ns)) {
-                        give_up(P.status, abort_flag, kSiteLoad);
-                        ok = false;
-                        break;
+                    if (!wait_all(empty(stage), phase ^ 1, kSiteLoad)) { ok = false; break; }
+                    if (lane == 0) {
+                        const uint32_t dst = stages_u32 + stage * G::kStageBytes;
+                        if (rank == 0) mbar_arrive_expect_tx(full(stage), bytes);
+                        if (kPair) {
+                            const uint32_t bar = bar0_leader + 8u * stage;
+                            tma_load_2d_pair(dst + kABytes, mw, bar, kb * kRowBytes, w_row, pol_w);
+                            if (!gather && rows > 0) tma_load_2d_pair(dst, ma, bar, kb * kRowBytes, a_row, pol_a);
+                        } else {
+                            tma_load_2d(dst + kABytes, mw, full(stage), kb * kRowBytes, w_row, pol_w);
+                            if (!gather) tma_load_2d(dst, ma, full(stage), kb * kRowBytes, a_row, pol_a);
+                        }
                     }
-                    const uint32_t dst = stages_u32 + stage * G::kStageBytes;
-                    if (rank == 0) mbar_arrive_expect_tx(full(stage), bytes);
-                    if (kPair) {
-                        const uint32_t bar = bar0_leader + 8u * stage;
-                        tma_load_2d_pair(dst + kABytes, mw, bar, kb * kRowBytes, w_row, pol_w);
-                        if (!gather && rows > 0) tma_load_2d_pair(dst, ma, bar, kb * kRowBytes, a_row, pol_a);
-                    } else {
-                        tma_load_2d(dst + kABytes, mw, full(stage), kb * kRowBytes, w_row, pol_w);
-                        if (!gather) tma_load_2d(dst, ma, full(stage), kb * kRowBytes, a_row, pol_a);
-                    }
+                    __syncwarp();
                     if (++stage == G::kStages) { stage = 0; phase ^= 1; }
                 }
             }
@@ -306,7 +321,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
             uint32_t phase = 0;
             bool ok = true;
             for (int u = worker; ok && u < un.total; u += workers) {
-                const Tile t = un.decode(u);
+                const Tile t = un.decode(u, P.E, P.N, G::kTileM);
                 const int rows = rows_of(t, rank);
                 const int base = t.r0 + static_cast<int>(rank) * kRowsPerCta;
                 int4 src = make_int4(0, 0, 0, 0);       // a row that is not there reads row 0, and is not used
@@ -315,14 +330,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
                     src = make_int4(pick(0), pick(1), pick(2), pick(3));
                 }
                 for (int kb = t.kb0; kb < t.kb1; ++kb) {
-                    // one lane waits for all (the outcome is shared), then every lane issues its own load
-                    int got = 1;
-                    if (lane == 0) got = mbar_wait(empty(stage), phase ^ 1, abort_flag, P.wait_ns);
-                    if (!__shfl_sync(0xffffffffu, got, 0)) {
-                        if (lane == 0) give_up(P.status, abort_flag, kSiteLoad);
-                        ok = false;
-                        break;
-                    }
+                    if (!wait_all(empty(stage), phase ^ 1, kSiteLoad)) { ok = false; break; }
                     if (4 * lane < rows) {
                         const uint32_t dst = stages_u32 + stage * G::kStageBytes + lane * 4 * kRowBytes;
                         if (kPair) tma_gather4_pair(dst, &M.a[0], bar0_leader + 8u * stage, kb * kRowBytes, src, pol_a);
@@ -331,39 +339,60 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
                     if (++stage == G::kStages) { stage = 0; phase ^= 1; }
                 }
             }
-        } else if (warp == 1 && lane == 0 && rank == 0) {
+        } else if (warp == 1 && rank == 0) {
             // ---- MMA issue ---------------------------------------------------------------------------------------
-            int stage = 0, b = 0;
-            uint32_t phase = 0, acc_phase = 0;
+            int stage = 0;
+            uint32_t phase = 0, n = 0;         // n: K blocks so far; block n uses accumulator n & 1
             bool ok = true;
-            for (int u = worker; ok && u < un.total; u += workers) {
-                const Tile t = un.decode(u);
+            for (int u = worker; u < un.total; u += workers) {
+                const Tile t = un.decode(u, P.E, P.N, G::kTileM);
                 const uint32_t idesc = idesc_e4m3(G::kTileM, t.cols <= kTileN / 2 ? kTileN / 2 : kTileN);
-                for (int kb = t.kb0; kb < t.kb1; ++kb) {
-                    if (!(kPair ? mbar_wait_cluster(acc_empty(b), acc_phase ^ 1, abort_flag, P.wait_ns)
-                                : mbar_wait(acc_empty(b), acc_phase ^ 1, abort_flag, P.wait_ns))) {
-                        give_up(P.status, abort_flag, kSiteMmaAcc);
-                        ok = false;
-                        break;
-                    }
-                    if (!(kPair ? mbar_wait_cluster(full(stage), phase, abort_flag, P.wait_ns)
-                                : mbar_wait(full(stage), phase, abort_flag, P.wait_ns))) {
-                        give_up(P.status, abort_flag, kSiteMmaOperands);
-                        ok = false;
-                        break;
+                for (int kb = t.kb0; kb < t.kb1; ++kb, ++n) {
+                    const int b = n & 1;
+                    // operands first: that wait passes while the blocks before are still being multiplied
+                    ok = ok && wait_all(full(stage), phase, kSiteMmaOperands);
+                    if (n >= 2) {
+                        named_sync(kBarEmpty + b, kEmptyThreads);
+                        if (kPair) ok = ok && wait_all(peer_empty(b), (n >> 1) - 1 & 1, kSiteMmaAcc);
                     }
                     tc_fence_after_sync();
-                    const uint64_t a = smem_desc_sw128(stages_u32 + stage * G::kStageBytes);
-                    const uint64_t w = smem_desc_sw128(stages_u32 + stage * G::kStageBytes + kABytes);
+                    if (ok && lane == 0) {
+                        const uint64_t a = smem_desc_sw128(stages_u32 + stage * G::kStageBytes);
+                        const uint64_t w = smem_desc_sw128(stages_u32 + stage * G::kStageBytes + kABytes);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {        // 32 of the block's 128 columns each
-                        if (kPair) umma_f8_pair(tmem_base + b * kTileN, a + 2 * k, w + 2 * k, idesc, k != 0);
-                        else umma_f8(tmem_base + b * kTileN, a + 2 * k, w + 2 * k, idesc, k != 0);
+                        for (int k = 0; k < 4; ++k)          // 32 of the block's 128 columns each
+                            umma_f8<kPair>(tmem_base + b * kTileN, a + 2 * k, w + 2 * k, idesc, k != 0);
+                        if (kPair) { umma_commit_pair(acc_full(b)); umma_commit_pair(empty(stage)); }
+                        else { umma_commit(acc_full(b)); umma_commit(empty(stage)); }
                     }
-                    if (kPair) { umma_commit_pair(empty(stage)); umma_commit_pair(acc_full(b)); }
-                    else { umma_commit(empty(stage)); umma_commit(acc_full(b)); }
+                    __syncwarp();
                     if (++stage == G::kStages) { stage = 0; phase ^= 1; }
-                    if (++b == 2) { b = 0; acc_phase ^= 1; }
+                }
+            }
+            for (uint32_t k = n < 2 ? 0 : n - 2; k < n; ++k) named_sync(kBarEmpty + (k & 1), kEmptyThreads);
+        } else if (warp == 1) {
+            // ---- the other CTA of a pair: tells the leader which accumulators its epilogue has read ----------------
+            uint32_t n = 0;
+            for (int u = worker; u < un.total; u += workers) {
+                const Tile t = un.decode(u, P.E, P.N, G::kTileM);
+                for (int kb = t.kb0; kb < t.kb1; ++kb, ++n) {
+                    named_sync(kBarEmpty + (n & 1), kEmptyThreads);
+                    if (lane == 0) mbar_arrive_relaxed_cluster(bar0_leader + 8u * (2 * G::kStages + 2 + (n & 1)));
+                }
+            }
+        } else if (warp == 3) {
+            // ---- finished accumulators: this warp alone polls their barriers and wakes the epilogue's ----------------
+            uint32_t n = 0;
+            for (int u = worker; u < un.total; u += workers) {
+                const Tile t = un.decode(u, P.E, P.N, G::kTileM);
+                for (int kb = t.kb0; kb < t.kb1; ++kb, ++n) {
+                    if (!mbar_wait(acc_full(n & 1), (n >> 1) & 1, abort_flag, P.wait_ns))
+                        give_up(P.status, abort_flag, kSiteEpilogue);      // (from here on every wait gives up at once)
+                    __syncwarp();
+                    tc_fence_after_sync();
+                    tc_fence_before_sync();
+                    named_arrive(kBarFull + 2 * (n & 1), kFullThreads);
+                    named_arrive(kBarFull + 2 * (n & 1) + 1, kFullThreads);
                 }
             }
         }
@@ -373,67 +402,85 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
         const int wg = (warp - 4) >> 2, quarter = warp & 3, wg_thread = tid - 128 - wg * 128;
         uint8_t* stage_out = staging + (warp - 4) * kStageWarpBytes;
         const uint32_t tmem_mine = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + wg * (kTileN / 2);
-        const uint32_t acc_empty_remote = kPair ? bar0_leader + 8u * (2 * G::kStages + 2) : 0u;
         const int nb = (P.N + kFp8Block - 1) / kFp8Block;
-        int b = 0;
-        uint32_t acc_phase = 0;
-        bool ok = true;
-        for (int u = worker; ok && u < un.total; u += workers) {
-            const Tile t = un.decode(u);
-            const int row0 = t.r0 + static_cast<int>(rank) * kRowsPerCta + quarter * 32;       // of the warp
-            const int warp_rows = min(max(rows_of(t, rank) - quarter * 32, 0), 32);
-            const int n0 = t.n0 + wg * (kTileN / 2);
-            const int cols = min(max(P.N - n0, 0), kTileN / 2);
-            const bool active = warp_rows > 0 && cols > 0;         // the same for all lanes
-            const bool mine = active && lane < warp_rows;
-            const int src = mine ? source_row(P, row0 + lane) : -1;
-            const float* xs = P.x_scale + (src >= 0 ? src * P.ld_x_scale : 0);
-            const float* ws = P.w_scale + (static_cast<int64_t>(t.e) * nb + n0 / kFp8Block) * un.kb_all;
-            uint64_t acc[64];
+        // What the stores need is worked out again after the sums are done: kept in registers through the loop over K it
+        // made the loop spill.
+        struct Part { int row0, warp_rows, n0, cols; };
+        const auto part_of = [&](const Tile& t) {
+            Part p;
+            p.row0 = t.r0 + static_cast<int>(rank) * kRowsPerCta + quarter * 32;       // of the warp
+            p.warp_rows = min(max(rows_of(t, rank) - quarter * 32, 0), 32);
+            p.n0 = t.n0 + wg * (kTileN / 2);
+            p.cols = min(max(P.N - p.n0, 0), kTileN / 2);
+            return p;
+        };
+        uint32_t n = 0;
+        for (int u = worker; u < un.total; u += workers) {
+            float acc[128];
 #pragma unroll
-            for (int i = 0; i < 64; ++i) acc[i] = 0;
-            float xs_next = 0.0f, ws_next = 0.0f;
-            if (active) { xs_next = xs[t.kb0]; ws_next = ws[t.kb0]; }
-            for (int kb = t.kb0; kb < t.kb1; ++kb) {
-                const float f = xs_next * ws_next;
-                if (active && kb + 1 < t.kb1) { xs_next = xs[kb + 1]; ws_next = ws[kb + 1]; }
-                if (!__all_sync(0xffffffffu, mbar_wait(acc_full(b), acc_phase, abort_flag, P.wait_ns))) {
-                    give_up(P.status, abort_flag, kSiteEpilogue);
-                    ok = false;
-                    break;
-                }
-                tc_fence_after_sync();
-                if (active) {
-                    const uint64_t f2 = pack2(__float_as_uint(f), __float_as_uint(f));
-                    uint32_t p0[32], p1[32];
-                    const uint32_t at = tmem_mine + b * kTileN;
-                    const auto add = [&](const uint32_t (&p)[32], int first_pair) {
-#pragma unroll
-                        for (int i = 0; i < 16; ++i) acc[first_pair + i] = fma2(pack2(p[2 * i], p[2 * i + 1]), f2, acc[first_pair + i]);
-                    };
-                    tmem_ld_32(at, p0);
-                    tmem_ld_wait();
-                    tmem_ld_32(at + 32, p1);
-                    add(p0, 0);
-                    tmem_ld_wait();
-                    tmem_ld_32(at + 64, p0);
-                    add(p1, 16);
-                    tmem_ld_wait();
-                    tmem_ld_32(at + 96, p1);
-                    add(p0, 32);
-                    tmem_ld_wait();
-                    tc_fence_before_sync();
-                    __syncwarp();
-                    if (lane == 0) {
-                        if (kPair) mbar_arrive_cluster(acc_empty_remote + 8u * b); else mbar_arrive(acc_empty(b));
+            for (int i = 0; i < 128; ++i) acc[i] = 0.0f;
+            {
+                const Tile t = un.decode(u, P.E, P.N, G::kTileM);
+                const Part pt = part_of(t);
+                const bool active = pt.warp_rows > 0 && pt.cols > 0;         // the same for all lanes
+                const int src = active && lane < pt.warp_rows ? source_row(P, pt.row0 + lane) : -1;
+                const float* xs = P.x_scale + (src >= 0 ? src * P.ld_x_scale : 0);
+                const float* ws = P.w_scale + (static_cast<int64_t>(t.e) * nb + pt.n0 / kFp8Block) * un.kb_all;
+                const int kb1 = t.kb1;
+                // Scales arrive long before they are needed and wait in registers, the row's four at a time.  A row's scales
+                // lie together and a warp's rows do not: 32 lines per load, which the load unit takes one by one while the
+                // barriers of the other warps queue behind it, so the loads are as few and as wide as alignment allows.
+                const auto load_xs = [&](int kb) {             // the aligned group of four that holds block kb
+                    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                    const int at = kb & ~3;
+                    if (!active || kb >= kb1) return v;
+                    if (P.xs_vec) return __ldg(reinterpret_cast<const float4*>(xs + at));
+                    v.x = __ldg(xs + at);
+                    if (at + 1 < un.kb_all) v.y = __ldg(xs + at + 1);
+                    if (at + 2 < un.kb_all) v.z = __ldg(xs + at + 2);
+                    if (at + 3 < un.kb_all) v.w = __ldg(xs + at + 3);
+                    return v;
+                };
+                int kb = t.kb0;
+                float4 xs_now = load_xs(kb), xs_next = load_xs((kb & ~3) + 4);
+                float ws_now = active ? __ldg(ws + kb) : 0.0f;
+                for (; kb < kb1; ++kb) {
+                    const float f = ((kb & 2) ? ((kb & 1) ? xs_now.w : xs_now.z) : ((kb & 1) ? xs_now.y : xs_now.x)) * ws_now;
+                    if (active && kb + 1 < kb1) ws_now = __ldg(ws + kb + 1);
+                    if ((kb & 3) == 3) {
+                        xs_now = xs_next;
+                        xs_next = load_xs(kb + 5);
                     }
-                    add(p1, 48);
-                } else if (lane == 0) {
-                    if (kPair) mbar_arrive_cluster(acc_empty_remote + 8u * b); else mbar_arrive(acc_empty(b));
+                    const int b = n++ & 1;
+                    named_sync(kBarFull + 2 * b + wg, kFullThreads);
+                    tc_fence_after_sync();
+                    if (active) {
+                        const uint32_t at = tmem_mine + b * kTileN;
+                        uint32_t p[32];
+#pragma unroll
+                        for (int c = 0; c < 4; ++c) {
+                            tmem_ld_32(at + 32 * c, p);
+                            tmem_ld_wait();
+                            if (c == 3) {
+                                tc_fence_before_sync();
+                                named_arrive(kBarEmpty + b, kEmptyThreads);
+                            }
+#pragma unroll
+                            for (int i = 0; i < 32; ++i) acc[c * 32 + i] = fmaf(__uint_as_float(p[i]), f, acc[c * 32 + i]);
+                        }
+                    } else {
+                        named_arrive(kBarEmpty + b, kEmptyThreads);
+                    }
                 }
-                if (++b == 2) { b = 0; acc_phase ^= 1; }
             }
-            if (!ok) break;
+            // (after a wait that gave up what follows stores numbers that mean nothing, to the places they belong to)
+            int again = u;
+            asm volatile("" : "+r"(again));
+            const Tile t = un.decode(again, P.E, P.N, G::kTileM);
+            const Part pt = part_of(t);
+            const int row0 = pt.row0, warp_rows = pt.warp_rows, n0 = pt.n0, cols = pt.cols;
+            const bool active = warp_rows > 0 && cols > 0, mine = active && lane < warp_rows;
+            const int src = mine ? source_row(P, row0 + lane) : -1;
 
             if (un.splits > 1) {
                 // leave the sums; the part that comes last collects all of them in the order of K.  Every warp keeps its own
@@ -444,42 +491,36 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
                                   (static_cast<size_t>(rank) * 2 + wg) * 32 * 128 + wg_thread;
 #pragma unroll
                 for (int i = 0; i < 32; ++i) {
-                    const float2 x = unpack2(acc[2 * i]), y = unpack2(acc[2 * i + 1]);
-                    __stcg(mine_at + i * 128, make_float4(x.x, x.y, y.x, y.y));
+                    __stcg(mine_at + i * 128, make_float4(acc[4 * i], acc[4 * i + 1], acc[4 * i + 2], acc[4 * i + 3]));
                 }
                 __threadfence();
                 __syncwarp();
-                int seen = 0;
+                int arrived = 0;
                 if (lane == 0) {
                     int32_t* ticket = P.tickets + (static_cast<int64_t>(t.tile) * 2 + rank) * 8 + (warp - 4);
-                    seen = atomicAdd(ticket, 1);
-                    if (seen == un.splits - 1) *ticket = 0;
+                    arrived = atomicAdd(ticket, 1);
+                    if (arrived == un.splits - 1) *ticket = 0;
                     __threadfence();
                 }
-                if (__shfl_sync(0xffffffffu, seen, 0) != un.splits - 1) continue;
+                if (__shfl_sync(0xffffffffu, arrived, 0) != un.splits - 1) continue;
 #pragma unroll
-                for (int i = 0; i < 64; ++i) acc[i] = 0;
+                for (int i = 0; i < 128; ++i) acc[i] = 0.0f;
                 const float4* part = mine_at - static_cast<size_t>(t.split) * unit_float4;
-                const uint64_t one2 = pack2(__float_as_uint(1.0f), __float_as_uint(1.0f));
                 for (int s = 0; s < un.splits; ++s) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
                         const float4 v = __ldcg(part + i * 128);
-                        acc[2 * i] = fma2(pack2(__float_as_uint(v.x), __float_as_uint(v.y)), one2, acc[2 * i]);
-                        acc[2 * i + 1] = fma2(pack2(__float_as_uint(v.z), __float_as_uint(v.w)), one2, acc[2 * i + 1]);
+                        acc[4 * i] += v.x;
+                        acc[4 * i + 1] += v.y;
+                        acc[4 * i + 2] += v.z;
+                        acc[4 * i + 3] += v.w;
                     }
                     part += unit_float4;
                 }
             }
             if (!active) continue;
 
-            float v[128];
-#pragma unroll
-            for (int i = 0; i < 64; ++i) {
-                const float2 x = unpack2(acc[i]);
-                v[2 * i] = x.x;
-                v[2 * i + 1] = x.y;
-            }
+            float (&v)[128] = acc;
             if (src < 0) {                       // no such row: zeros, whatever the gathered stand-in held
 #pragma unroll
                 for (int i = 0; i < 128; ++i) v[i] = 0.0f;
@@ -639,6 +680,7 @@ int matmul(const monde_matmul_problem* p, const void* x, const float* x_scale, c
     P.row_ids = row_ids;
     P.out = out;
     P.out_scale = out_scale;
+    P.xs_vec = aligned(x_scale, 16) && p->ld_x_scale % 4 == 0 && ((p->K + kFp8Block - 1) / kFp8Block) % 4 == 0;
     P.out_vec = aligned(out, 16) && (p->ld_out * ob) % 16 == 0;
     P.status = reinterpret_cast<int32_t*>(base + WsLayout::kStatus);
     P.tickets = reinterpret_cast<int32_t*>(base + WsLayout::kPartDone);
