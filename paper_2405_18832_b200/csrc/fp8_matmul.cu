@@ -48,7 +48,7 @@ struct MatmulMaps {
     CUtensorMap w[2];       // the columns of a full and of a half tile
 };
 
-constexpr int kThreads = 384;          // warps 0-3: weight loads, MMA, row loads, spare; warps 4-11: two epilogue warpgroups
+constexpr int kThreads = 384;          // warps 0-3: loads, MMA, MMA, polling; warps 4-11: two epilogue warpgroups
 constexpr int kTileN = 256;
 // Hardware barriers.  Full: an accumulator is finished (the polling warp and one epilogue warpgroup, [buffer][warpgroup]).
 // Empty: it has been read (both warpgroups and the MMA warp).  With every epilogue warp polling the mbarriers themselves,
@@ -119,6 +119,7 @@ template <bool kPair> struct Geometry {
     static constexpr int kBBytes = (kPair ? 128 : 256) * kRowBytes;   // weight rows a CTA loads
     static constexpr int kStageBytes = kABytes + kBBytes;
     static constexpr int kStages = kPair ? 6 : 4;
+    static_assert(kStages % 2 == 0, "the MMA warps take every other stage");
     static constexpr int kBars = 2 * kStages + 4;
     static constexpr int kSmem = 1024 + kStages * kStageBytes + 8 * kStageWarpBytes + kBars * 8 + 64 + static_cast<int>(sizeof(Units));
 };
@@ -278,9 +279,9 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
     };
 
     if (warp < 4) {
-        regs_dec<40>();
+        regs_dec<56>();
         if (warp == 0) {
-            // ---- loads of weights and of contiguous rows ---------------------------------------------------------
+            // ---- loads: weights and contiguous rows by one lane, rows picked by id by every lane four --------------------
             const uint64_t pol_w = policy_evict_first(), pol_a = policy_evict_last();
             int stage = 0;
             uint32_t phase = 0;
@@ -296,64 +297,51 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
                                        (kPair ? 2 : 1) * b_rows * kRowBytes;
                 const int w_row = t.e * P.N + t.n0 + static_cast<int>(rank) * b_rows;
                 const int a_row = t.r0 + static_cast<int>(rank) * kRowsPerCta;
+                int4 src = make_int4(0, 0, 0, 0);       // a row that is not there reads row 0, and is not used
+                const bool gathers = gather && 4 * lane < rows;
+                if (gathers) {
+                    const auto pick = [&](int j) { return 4 * lane + j < rows ? max(source_row(P, a_row + 4 * lane + j), 0) : 0; };
+                    src = make_int4(pick(0), pick(1), pick(2), pick(3));
+                }
                 for (int kb = t.kb0; kb < t.kb1; ++kb) {
                     if (!wait_all(empty(stage), phase ^ 1, kSiteLoad)) { ok = false; break; }
+                    const uint32_t dst = stages_u32 + stage * G::kStageBytes, bar = bar0_leader + 8u * stage;
                     if (lane == 0) {
-                        const uint32_t dst = stages_u32 + stage * G::kStageBytes;
                         if (rank == 0) mbar_arrive_expect_tx(full(stage), bytes);
                         if (kPair) {
-                            const uint32_t bar = bar0_leader + 8u * stage;
                             tma_load_2d_pair(dst + kABytes, mw, bar, kb * kRowBytes, w_row, pol_w);
                             if (!gather && rows > 0) tma_load_2d_pair(dst, ma, bar, kb * kRowBytes, a_row, pol_a);
                         } else {
-                            tma_load_2d(dst + kABytes, mw, full(stage), kb * kRowBytes, w_row, pol_w);
-                            if (!gather) tma_load_2d(dst, ma, full(stage), kb * kRowBytes, a_row, pol_a);
+                            tma_load_2d(dst + kABytes, mw, bar, kb * kRowBytes, w_row, pol_w);
+                            if (!gather) tma_load_2d(dst, ma, bar, kb * kRowBytes, a_row, pol_a);
                         }
+                    }
+                    if (gathers) {
+                        if (kPair) tma_gather4_pair(dst + lane * 4 * kRowBytes, &M.a[0], bar, kb * kRowBytes, src, pol_a);
+                        else tma_gather4(dst + lane * 4 * kRowBytes, &M.a[0], bar, kb * kRowBytes, src, pol_a);
                     }
                     __syncwarp();
                     if (++stage == G::kStages) { stage = 0; phase ^= 1; }
                 }
             }
-        } else if (warp == 2 && gather) {
-            // ---- loads of rows picked by id: every lane four rows ------------------------------------------------
-            const uint64_t pol_a = policy_evict_last();
-            int stage = 0;
-            uint32_t phase = 0;
-            bool ok = true;
-            for (int u = worker; ok && u < un.total; u += workers) {
-                const Tile t = un.decode(u, P.E, P.N, G::kTileM);
-                const int rows = rows_of(t, rank);
-                const int base = t.r0 + static_cast<int>(rank) * kRowsPerCta;
-                int4 src = make_int4(0, 0, 0, 0);       // a row that is not there reads row 0, and is not used
-                if (4 * lane < rows) {
-                    const auto pick = [&](int j) { return 4 * lane + j < rows ? max(source_row(P, base + 4 * lane + j), 0) : 0; };
-                    src = make_int4(pick(0), pick(1), pick(2), pick(3));
-                }
-                for (int kb = t.kb0; kb < t.kb1; ++kb) {
-                    if (!wait_all(empty(stage), phase ^ 1, kSiteLoad)) { ok = false; break; }
-                    if (4 * lane < rows) {
-                        const uint32_t dst = stages_u32 + stage * G::kStageBytes + lane * 4 * kRowBytes;
-                        if (kPair) tma_gather4_pair(dst, &M.a[0], bar0_leader + 8u * stage, kb * kRowBytes, src, pol_a);
-                        else tma_gather4(dst, &M.a[0], full(stage), kb * kRowBytes, src, pol_a);
-                    }
-                    if (++stage == G::kStages) { stage = 0; phase ^= 1; }
-                }
-            }
-        } else if (warp == 1 && rank == 0) {
-            // ---- MMA issue ---------------------------------------------------------------------------------------
-            int stage = 0;
+        } else if ((warp == 1 || warp == 2) && rank == 0) {
+            // ---- MMA issue: two warps take turns, one accumulator each -------------------------------------------------
+            // Issuing a block's four MMAs takes the warp as long as the tensor core takes to run them, and its waits add some
+            // 350 cycles: with one warp the tensor core stood still for those.
+            const int b = warp - 1;
+            int stage = b;
             uint32_t phase = 0, n = 0;         // n: K blocks so far; block n uses accumulator n & 1
             bool ok = true;
             for (int u = worker; u < un.total; u += workers) {
                 const Tile t = un.decode(u, P.E, P.N, G::kTileM);
                 const uint32_t idesc = idesc_e4m3(G::kTileM, t.cols <= kTileN / 2 ? kTileN / 2 : kTileN);
                 for (int kb = t.kb0; kb < t.kb1; ++kb, ++n) {
-                    const int b = n & 1;
+                    if ((n & 1) != b) continue;
                     // operands first: that wait passes while the blocks before are still being multiplied
                     ok = ok && wait_all(full(stage), phase, kSiteMmaOperands);
                     if (n >= 2) {
                         named_sync(kBarEmpty + b, kEmptyThreads);
-                        if (kPair) ok = ok && wait_all(peer_empty(b), (n >> 1) - 1 & 1, kSiteMmaAcc);
+                        if (kPair) ok = ok && wait_all(peer_empty(b), ((n >> 1) - 1) & 1, kSiteMmaAcc);
                     }
                     tc_fence_after_sync();
                     if (ok && lane == 0) {
@@ -366,10 +354,10 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
                         else { umma_commit(acc_full(b)); umma_commit(empty(stage)); }
                     }
                     __syncwarp();
-                    if (++stage == G::kStages) { stage = 0; phase ^= 1; }
+                    if ((stage += 2) >= G::kStages) { stage -= G::kStages; phase ^= 1; }
                 }
             }
-            for (uint32_t k = n < 2 ? 0 : n - 2; k < n; ++k) named_sync(kBarEmpty + (k & 1), kEmptyThreads);
+            if (n > static_cast<uint32_t>(b)) named_sync(kBarEmpty + b, kEmptyThreads);      // the last block's
         } else if (warp == 1) {
             // ---- the other CTA of a pair: tells the leader which accumulators its epilogue has read ----------------
             uint32_t n = 0;
@@ -398,7 +386,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
         }
     } else {
         // ---- epilogue: scale and add the blocks, then bias, activation, rounding and stores ----------------------
-        regs_inc<232>();
+        regs_inc<224>();
         const int wg = (warp - 4) >> 2, quarter = warp & 3, wg_thread = tid - 128 - wg * 128;
         uint8_t* stage_out = staging + (warp - 4) * kStageWarpBytes;
         const uint32_t tmem_mine = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + wg * (kTileN / 2);
