@@ -23,10 +23,28 @@ __device__ __forceinline__ float max_nan(float a, float b) {
 __device__ __forceinline__ float block_scale(float amax) {
     return amax < kTinyAmax ? 1.0f : __fdiv_rn(amax, kE4m3Max);
 }
-// Activations as in the bf16 layer, but a NaN stays one (relu by fmaxf would turn a poisoned block into zeros).
-__device__ __forceinline__ float apply_act_nan(float v, int act) {
-    if (act == MONDE_ACT_NONE) return v;
-    return act == MONDE_ACT_RELU ? max_nan(v, 0.0f) : apply_act(v, MONDE_ACT_GELU_ERF);
+// v * Phi(v) for two values, Phi the normal distribution function: gelu(v) = max(v, 0) - |v| * Phi(-|v|), and
+// log2 Phi(-z) is so close to a parabola that a polynomial of degree 9 gives it on [0, 13.5] (past that Phi(-z) is below the
+// smallest normal number) with an absolute error of Phi below 1e-7, the size of a rounding of the result's factor.  Fitted by
+// weighted least squares to log2 of the normal distribution function.  One exponential and packed additions, a third of the
+// time of the error function's.  A NaN stays one.
+__device__ __forceinline__ float2 gelu2(float2 v) {
+    const float2 z = make_float2(fminf(fabsf(v.x), 13.5f), fminf(fabsf(v.y), 13.5f));
+    const auto step = [&](float2 r, float c) { return __ffma2_rn(r, z, make_float2(c, c)); };
+    float2 r = make_float2(2.034508916892719e-08f, 2.034508916892719e-08f);
+    r = step(r, -8.277030474346248e-07f);
+    r = step(r, 1.1681644537020475e-05f);
+    r = step(r, -4.732228990178555e-05f);
+    r = step(r, -0.0004760378214996308f);
+    r = step(r, 0.007496591191738844f);
+    r = step(r, -0.05278078094124794f);
+    r = step(r, -0.45912107825279236f);
+    r = step(r, -1.1511149406433105f);
+    r = step(r, -0.9999998211860657f);
+    float2 q;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(q.x) : "f"(r.x));
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(q.y) : "f"(r.y));
+    return make_float2(fmaf(-z.x, q.x, max_nan(v.x, 0.0f)), fmaf(-z.y, q.y, max_nan(v.y, 0.0f)));
 }
 // Four values to e4m3, round to nearest even; the largest of a block lands on 448 (one rounding step of the product above
 // it at most, which rounds back), so nothing saturates.

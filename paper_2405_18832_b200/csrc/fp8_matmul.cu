@@ -14,6 +14,8 @@
 // adds them in the order of K, whoever it is, so results are bit-reproducible and nobody waits.
 #include <cuda.h>
 
+#include <type_traits>
+
 #include "fp8.cuh"
 #include "sm100.cuh"
 
@@ -33,8 +35,8 @@ struct MatmulParams {
     const int32_t* row_ids;     // null: position r reads row r
     void* out;
     float* out_scale;
-    int xs_vec;                 // rows of x_scale: 16-byte boundaries and whole groups of four
-    int out_vec;                // rows of `out` start on 16-byte boundaries
+    int out_vec;                // rows of `out` start on 32-byte boundaries
+    int bias_vec;               // rows of `bias` start on 16-byte boundaries
     int32_t* status;            // {status, site}
     int32_t* tickets;           // [tile][CTA of the pair][epilogue warp]: parts of a K-split tile that have finished (zero between calls)
     float4* partials;           // [unit][CTA of the pair][column half][32][128 threads]
@@ -60,8 +62,9 @@ constexpr int kABytes = kRowsPerCta * kRowBytes;
 constexpr int kMaxSplit = 16;
 constexpr int kMaxSplitUnits = 296;    // units of a K-split product: bounds the workspace
 constexpr size_t kUnitPartialBytes = size_t(kRowsPerCta) * kTileN * 4;
-constexpr int kStagePitch = 80;        // output staging: 64 bytes of a row, padded so that 8 lanes' 16-byte writes miss one another's banks
-constexpr int kStageWarpBytes = 32 * kStagePitch;
+constexpr int kStageWarpBytes = 32 * 16;                            // output rows that cannot go out straight
+constexpr int kScalePitch = 9, kScaleHalf = 33 * kScalePitch;        // scales of eight K blocks: 32 rows and the weights'
+constexpr int kScaleWarpBytes = 2 * kScaleHalf * 4;
 constexpr int kRowGroup = 8;           // row tiles that go together through the columns
 
 
@@ -84,44 +87,43 @@ struct Tile {
 struct Units {
     int total, splits;              // units; parts per tile
     int n_tiles, kb_all;            // 256-column tiles of a row tile; K blocks
+    uint32_t inverse[kMaxSplit + 1];    // ceil(2^32 / d)
     int prefix[kMaxExperts + 1];    // row tiles of the experts before e
     int first[kMaxExperts + 1];     // first row of expert e
-    __device__ __forceinline__ Tile decode(int u, int E, int N, int tile_m) const {
+    // Whole warps call.  (Divisions by numbers up to 16 are products with ceil(2^32 / d), exact below 2^28.)
+    __device__ __forceinline__ Tile decode(int u, int lane, int E, int N, int tile_m) const {
         Tile t;
-        t.tile = u / splits;
-        t.split = u - t.tile * splits;
-        int lo = 0, hi = E - 1;                       // largest e with prefix[e] * n_tiles <= tile (empty experts have no tiles)
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (prefix[mid] * n_tiles <= t.tile) lo = mid; else hi = mid - 1;
+        const int parts = splits;
+        t.tile = parts == 1 ? u : static_cast<int>(__umulhi(u, small_inverse(parts)));
+        t.split = u - t.tile * parts;
+        // the expert: the last one with prefix[e] * n_tiles <= tile (experts without rows have no tiles), by two ballots
+        const int tiles = n_tiles;
+        const int coarse = __popc(__ballot_sync(0xffffffffu, lane * 8 < E && prefix[min(lane * 8, E)] * tiles <= t.tile)) - 1;
+        const int at = coarse * 8 + (lane & 7);
+        const unsigned fine = __ballot_sync(0xffffffffu, at < E && prefix[min(at, E)] * tiles <= t.tile);
+        t.e = coarse * 8 + __popc(fine & 0xffu) - 1;
+        const int first_tile = prefix[t.e], m_tiles = prefix[t.e + 1] - first_tile;
+        int local = t.tile - first_tile * tiles, g = 0;
+        if (m_tiles > kRowGroup) {
+            g = local / (kRowGroup * tiles);
+            local -= g * kRowGroup * tiles;
         }
-        t.e = lo;
-        const int m_tiles = prefix[lo + 1] - prefix[lo];
-        int local = t.tile - prefix[lo] * n_tiles;
-        const int per_group = kRowGroup * n_tiles;
-        const int g = local / per_group;
-        local -= g * per_group;
         const int in_group = min(kRowGroup, m_tiles - g * kRowGroup);
-        const int n = local / in_group;
+        const int n = in_group == 1 ? local : static_cast<int>(__umulhi(local, small_inverse(in_group)));
         const int m = g * kRowGroup + local - n * in_group;
-        t.r0 = first[lo] + m * tile_m;
-        t.rows = min(tile_m, first[lo + 1] - t.r0);
+        t.r0 = first[t.e] + m * tile_m;
+        t.rows = min(tile_m, first[t.e + 1] - t.r0);
         t.n0 = n * kTileN;
         t.cols = min(kTileN, N - t.n0);
-        t.kb0 = static_cast<unsigned>(kb_all * t.split) / splits;          // (K < 2^31, at most 16 parts: no overflow)
-        t.kb1 = static_cast<unsigned>(kb_all * (t.split + 1)) / splits;
+        t.kb0 = 0;
+        t.kb1 = kb_all;
+        if (parts > 1) {                     // (K < 2^31, at most 16 parts: no overflow)
+            t.kb0 = static_cast<int>(__umulhi(kb_all * t.split, small_inverse(parts)));
+            t.kb1 = static_cast<int>(__umulhi(kb_all * (t.split + 1), small_inverse(parts)));
+        }
         return t;
     }
-};
-
-template <bool kPair> struct Geometry {
-    static constexpr int kTileM = kPair ? 256 : 128;              // rows of a tile (a pair: 128 in each CTA)
-    static constexpr int kBBytes = (kPair ? 128 : 256) * kRowBytes;   // weight rows a CTA loads
-    static constexpr int kStageBytes = kABytes + kBBytes;
-    static constexpr int kStages = kPair ? 6 : 4;
-    static_assert(kStages % 2 == 0, "the MMA warps take every other stage");
-    static constexpr int kBars = 2 * kStages + 4;
-    static constexpr int kSmem = 1024 + kStages * kStageBytes + 8 * kStageWarpBytes + kBars * 8 + 64 + static_cast<int>(sizeof(Units));
+    __device__ __forceinline__ uint32_t small_inverse(int d) const { return inverse[d]; }
 };
 
 // Parts of the K range: as many as shorten the longest CTA's work, counted in K blocks, where a split tile pays about
@@ -135,43 +137,55 @@ __device__ __forceinline__ int choose_splits(int tiles, int workers, int kb_all)
     return best;
 }
 
-__device__ __forceinline__ int source_row(const MatmulParams& P, int r) {      // -1: no such row
-    if (P.row_ids == nullptr) return r;
-    const int id = P.row_ids[r];
+template <bool kPair> struct Geometry {
+    static constexpr int kTileM = kPair ? 256 : 128;              // rows of a tile (a pair: 128 in each CTA)
+    static constexpr int kBBytes = (kPair ? 128 : 256) * kRowBytes;   // weight rows a CTA loads
+    static constexpr int kStageBytes = kABytes + kBBytes;
+    static constexpr int kStages = kPair ? 6 : 4;
+    static_assert(kStages % 2 == 0, "the MMA warps take every other stage");
+    static constexpr int kBars = 2 * kStages + 4;
+    static constexpr int kSmem = 1024 + kStages * kStageBytes + 8 * (kStageWarpBytes + kScaleWarpBytes) + kBars * 8 + 64 + static_cast<int>(sizeof(Units));
+};
+
+// The row of x that output row r reads, in two steps so that the load can be issued long before its answer is needed.
+__device__ __forceinline__ int load_row_id(const MatmulParams& P, int r) { return P.row_ids != nullptr ? P.row_ids[r] : r; }
+__device__ __forceinline__ int source_row(const MatmulParams& P, int id) {      // -1: no such row
+    if (P.row_ids == nullptr) return id;
     const int s = id < 0 ? -1 : id / P.row_div;
     return s < P.src_rows ? s : -1;
 }
 
-// 128 columns of 32 rows (a row per lane) to global memory, 64 bytes of each row at a time through shared memory, so that
-// stores are 64-byte runs of a row.  `word(i)`: 32-bit word i of this lane's row.
+// 128 columns of 32 rows, a row per lane, to global memory; `word(i)`: 32-bit word i of this lane's row.  Whole tiles whose
+// rows start on 32-byte boundaries go out straight from registers, a sector per lane and store; others 16 bytes of each row
+// at a time through shared memory, element by element.
 template <int kEsize, typename F>
 __device__ __forceinline__ void store_rows(uint8_t* stage, uint8_t* out_row0, int64_t ld_bytes, int rows, int cols,
                                            bool vec, int lane, F word) {
-    constexpr int kPasses = 128 * kEsize / 64;
-    const int bytes = cols * kEsize;
+    if (vec && cols == kFp8Block) {
+        if (lane < rows) {
+            uint8_t* dst = out_row0 + lane * ld_bytes;
 #pragma unroll
-    for (int p = 0; p < kPasses; ++p) {
-        __syncwarp();
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-            *reinterpret_cast<uint4*>(stage + lane * kStagePitch + c * 16) =
-                make_uint4(word(p * 16 + c * 4), word(p * 16 + c * 4 + 1), word(p * 16 + c * 4 + 2), word(p * 16 + c * 4 + 3));
-        __syncwarp();
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const int row = i * 8 + (lane >> 2), at = p * 64 + (lane & 3) * 16;
-            if (row >= rows || at >= bytes) continue;
-            const uint8_t* src = stage + row * kStagePitch + (lane & 3) * 16;
-            uint8_t* dst = out_row0 + row * ld_bytes + at;
-            if (vec && at + 16 <= bytes) {
-                *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<const uint4*>(src);
-            } else {
-                for (int j = 0; j < 16 && at + j < bytes; j += kEsize) {
-                    if constexpr (kEsize == 1) dst[j] = src[j];
-                    else if constexpr (kEsize == 2) *reinterpret_cast<uint16_t*>(dst + j) = *reinterpret_cast<const uint16_t*>(src + j);
-                    else *reinterpret_cast<uint32_t*>(dst + j) = *reinterpret_cast<const uint32_t*>(src + j);
-                }
+            for (int p = 0; p < kEsize * 4; ++p) {
+                const uint32_t w[8] = {word(p * 8), word(p * 8 + 1), word(p * 8 + 2), word(p * 8 + 3),
+                                       word(p * 8 + 4), word(p * 8 + 5), word(p * 8 + 6), word(p * 8 + 7)};
+                store_32(dst + p * 32, w);
             }
+        }
+        return;
+    }
+    using E = std::conditional_t<kEsize == 1, uint8_t, std::conditional_t<kEsize == 2, uint16_t, uint32_t>>;
+    constexpr int kPer = 16 / kEsize;             // elements of a row in one pass
+#pragma unroll
+    for (int p = 0; p < kEsize * 8; ++p) {
+        if (p * kPer >= cols) break;
+        __syncwarp();
+        *reinterpret_cast<uint4*>(stage + lane * 16) = make_uint4(word(p * 4), word(p * 4 + 1), word(p * 4 + 2), word(p * 4 + 3));
+        __syncwarp();
+        const int n = min(kPer, cols - p * kPer);
+#pragma unroll 1
+        for (int i = lane; i < rows * kPer; i += 32) {
+            const int row = i / kPer, col = i % kPer;
+            if (col < n) reinterpret_cast<E*>(out_row0 + row * ld_bytes)[p * kPer + col] = reinterpret_cast<const E*>(stage)[i];
         }
     }
 }
@@ -182,7 +196,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
     uint8_t* staging = smem + G::kStages * G::kStageBytes;
-    uint64_t* bars = reinterpret_cast<uint64_t*>(staging + 8 * kStageWarpBytes);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(staging + 8 * (kStageWarpBytes + kScaleWarpBytes));
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + G::kBars);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     Units& un = *reinterpret_cast<Units*>(tmem_slot + 16);
@@ -244,6 +258,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
     }
     const int workers = kPair ? static_cast<int>(gridDim.x) / 2 : static_cast<int>(gridDim.x);
     const int worker = kPair ? static_cast<int>(blockIdx.x) / 2 : static_cast<int>(blockIdx.x);
+    if (tid >= 2 && tid <= kMaxSplit) un.inverse[tid] = 0xffffffffu / static_cast<uint32_t>(tid) + 1;
     if (warp == 0) {
         __syncwarp();
         if (lane == 0) {
@@ -278,6 +293,20 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
         return false;
     };
 
+    // K blocks of all of this CTA's units.
+    const auto count_blocks = [&]() {
+        uint32_t n = 0;
+        if (un.splits == 1) {
+            if (worker < un.total) n = static_cast<uint32_t>((un.total - 1 - worker) / workers + 1) * un.kb_all;
+        } else {
+            for (int u = worker; u < un.total; u += workers) {
+                const Tile t = un.decode(u, lane, P.E, P.N, G::kTileM);
+                n += t.kb1 - t.kb0;
+            }
+        }
+        return n;
+    };
+
     if (warp < 4) {
         regs_dec<56>();
         if (warp == 0) {
@@ -286,8 +315,20 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
             int stage = 0;
             uint32_t phase = 0;
             bool ok = true;
+            // the next tile is found, and its row ids are asked for, before this one's loads are issued
+            Tile next = {};
+            int4 ids = make_int4(0, 0, 0, 0);
+            const auto look_ahead = [&](int u) {
+                if (u >= un.total) return;
+                next = un.decode(u, lane, P.E, P.N, G::kTileM);
+                const int rows = rows_of(next, rank), r = next.r0 + static_cast<int>(rank) * kRowsPerCta + 4 * lane;
+                if (gather && 4 * lane < rows)
+                    ids = make_int4(P.row_ids[r], 4 * lane + 1 < rows ? P.row_ids[r + 1] : 0,
+                                    4 * lane + 2 < rows ? P.row_ids[r + 2] : 0, 4 * lane + 3 < rows ? P.row_ids[r + 3] : 0);
+            };
+            look_ahead(worker);
             for (int u = worker; ok && u < un.total; u += workers) {
-                const Tile t = un.decode(u, P.E, P.N, G::kTileM);
+                const Tile t = next;
                 const int rows = rows_of(t, rank);
                 const bool half = t.cols <= kTileN / 2;
                 const CUtensorMap* mw = &M.w[half];
@@ -297,12 +338,12 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
                                        (kPair ? 2 : 1) * b_rows * kRowBytes;
                 const int w_row = t.e * P.N + t.n0 + static_cast<int>(rank) * b_rows;
                 const int a_row = t.r0 + static_cast<int>(rank) * kRowsPerCta;
-                int4 src = make_int4(0, 0, 0, 0);       // a row that is not there reads row 0, and is not used
                 const bool gathers = gather && 4 * lane < rows;
-                if (gathers) {
-                    const auto pick = [&](int j) { return 4 * lane + j < rows ? max(source_row(P, a_row + 4 * lane + j), 0) : 0; };
-                    src = make_int4(pick(0), pick(1), pick(2), pick(3));
-                }
+                int4 src = make_int4(0, 0, 0, 0);       // a row that is not there reads row 0, and is not used
+                if (gathers)
+                    src = make_int4(max(source_row(P, ids.x), 0), max(source_row(P, ids.y), 0), max(source_row(P, ids.z), 0),
+                                    max(source_row(P, ids.w), 0));
+                look_ahead(u + workers);
                 for (int kb = t.kb0; kb < t.kb1; ++kb) {
                     if (!wait_all(empty(stage), phase ^ 1, kSiteLoad)) { ok = false; break; }
                     const uint32_t dst = stages_u32 + stage * G::kStageBytes, bar = bar0_leader + 8u * stage;
@@ -332,10 +373,13 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
             int stage = b;
             uint32_t phase = 0, n = 0;         // n: K blocks so far; block n uses accumulator n & 1
             bool ok = true;
+            Tile t = un.decode(worker, lane, P.E, P.N, G::kTileM);
             for (int u = worker; u < un.total; u += workers) {
-                const Tile t = un.decode(u, P.E, P.N, G::kTileM);
                 const uint32_t idesc = idesc_e4m3(G::kTileM, t.cols <= kTileN / 2 ? kTileN / 2 : kTileN);
-                for (int kb = t.kb0; kb < t.kb1; ++kb, ++n) {
+                const int blocks = t.kb1 - t.kb0;
+                // (the next tile is found while this one's first blocks are multiplied)
+                for (int i = 0; i < blocks; ++i, ++n) {
+                    if (i == min(2, blocks - 1) && u + workers < un.total) t = un.decode(u + workers, lane, P.E, P.N, G::kTileM);
                     if ((n & 1) != b) continue;
                     // operands first: that wait passes while the blocks before are still being multiplied
                     ok = ok && wait_all(full(stage), phase, kSiteMmaOperands);
@@ -360,28 +404,22 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
             if (n > static_cast<uint32_t>(b)) named_sync(kBarEmpty + b, kEmptyThreads);      // the last block's
         } else if (warp == 1) {
             // ---- the other CTA of a pair: tells the leader which accumulators its epilogue has read ----------------
-            uint32_t n = 0;
-            for (int u = worker; u < un.total; u += workers) {
-                const Tile t = un.decode(u, P.E, P.N, G::kTileM);
-                for (int kb = t.kb0; kb < t.kb1; ++kb, ++n) {
-                    named_sync(kBarEmpty + (n & 1), kEmptyThreads);
-                    if (lane == 0) mbar_arrive_relaxed_cluster(bar0_leader + 8u * (2 * G::kStages + 2 + (n & 1)));
-                }
+            const uint32_t total = count_blocks();
+            for (uint32_t n = 0; n < total; ++n) {
+                named_sync(kBarEmpty + (n & 1), kEmptyThreads);
+                if (lane == 0) mbar_arrive_relaxed_cluster(bar0_leader + 8u * (2 * G::kStages + 2 + (n & 1)));
             }
         } else if (warp == 3) {
             // ---- finished accumulators: this warp alone polls their barriers and wakes the epilogue's ----------------
-            uint32_t n = 0;
-            for (int u = worker; u < un.total; u += workers) {
-                const Tile t = un.decode(u, P.E, P.N, G::kTileM);
-                for (int kb = t.kb0; kb < t.kb1; ++kb, ++n) {
-                    if (!mbar_wait(acc_full(n & 1), (n >> 1) & 1, abort_flag, P.wait_ns))
-                        give_up(P.status, abort_flag, kSiteEpilogue);      // (from here on every wait gives up at once)
-                    __syncwarp();
-                    tc_fence_after_sync();
-                    tc_fence_before_sync();
-                    named_arrive(kBarFull + 2 * (n & 1), kFullThreads);
-                    named_arrive(kBarFull + 2 * (n & 1) + 1, kFullThreads);
-                }
+            const uint32_t total = count_blocks();
+            for (uint32_t n = 0; n < total; ++n) {
+                if (!mbar_wait(acc_full(n & 1), (n >> 1) & 1, abort_flag, P.wait_ns))
+                    give_up(P.status, abort_flag, kSiteEpilogue);      // (from here on every wait gives up at once)
+                __syncwarp();
+                tc_fence_after_sync();
+                tc_fence_before_sync();
+                named_arrive(kBarFull + 2 * (n & 1), kFullThreads);
+                named_arrive(kBarFull + 2 * (n & 1) + 1, kFullThreads);
             }
         }
     } else {
@@ -389,87 +427,107 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
         regs_inc<224>();
         const int wg = (warp - 4) >> 2, quarter = warp & 3, wg_thread = tid - 128 - wg * 128;
         uint8_t* stage_out = staging + (warp - 4) * kStageWarpBytes;
+        float* const scale_buf = reinterpret_cast<float*>(staging + 8 * kStageWarpBytes + (warp - 4) * kScaleWarpBytes);
         const uint32_t tmem_mine = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + wg * (kTileN / 2);
         const int nb = (P.N + kFp8Block - 1) / kFp8Block;
-        // What the stores need is worked out again after the sums are done: kept in registers through the loop over K it
-        // made the loop spill.
-        struct Part { int row0, warp_rows, n0, cols; };
+        struct Part { int row0, warp_rows, n0, cols, e, kb0, kb1; };
         const auto part_of = [&](const Tile& t) {
             Part p;
             p.row0 = t.r0 + static_cast<int>(rank) * kRowsPerCta + quarter * 32;       // of the warp
             p.warp_rows = min(max(rows_of(t, rank) - quarter * 32, 0), 32);
             p.n0 = t.n0 + wg * (kTileN / 2);
             p.cols = min(max(P.N - p.n0, 0), kTileN / 2);
+            p.e = t.e;
+            p.kb0 = t.kb0;
+            p.kb1 = t.kb1;
             return p;
         };
+        // The scales of eight K blocks lie in a buffer of the warp, [32 rows + the weights'][8, padded to 9], those of the next
+        // eight (of the next tile, at the end) are on their way to its other half.  Eight lanes read a row's scales: four
+        // lines per load, where a lane per row took 32, one after the other, with the barriers of the other warps behind.
+        int half = 0;
+        const auto load_scales = [&](const Part& p, int src, int kb, int to) {
+            const int at = kb + (lane & 7);
+            const bool active = p.warp_rows > 0 && p.cols > 0;
+            float* const dst = scale_buf + to * kScaleHalf + (lane & 7);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int r = 4 * j + (lane >> 3), s = __shfl_sync(0xffffffffu, src, r);
+                if (s >= 0 && at < p.kb1) copy_async_4(dst + r * kScalePitch, P.x_scale + s * P.ld_x_scale + at);
+            }
+            if (lane < 8 && active && at < p.kb1)
+                copy_async_4(dst + 32 * kScalePitch, P.w_scale + (static_cast<int64_t>(p.e) * nb + p.n0 / kFp8Block) * un.kb_all + at);
+            copy_async_commit();
+        };
+        // A tile is found, and its row ids are asked for, one tile ahead.
+        Part next = {};
+        int next_id = 0;
+        const auto look_ahead = [&](int u) {
+            if (u >= un.total) return;
+            next = part_of(un.decode(u, lane, P.E, P.N, G::kTileM));
+            if (next.cols > 0 && lane < next.warp_rows) next_id = load_row_id(P, next.row0 + lane);
+        };
+        const auto next_source = [&]() { return next.cols > 0 && lane < next.warp_rows ? source_row(P, next_id) : -1; };
+        look_ahead(worker);
+        int src = next_source();
+        if (worker < un.total) load_scales(next, src, next.kb0, 0);
         uint32_t n = 0;
         for (int u = worker; u < un.total; u += workers) {
+            const Part t = next;
+            const int row0 = t.row0, warp_rows = t.warp_rows, n0 = t.n0, cols = t.cols;
+            const bool active = warp_rows > 0 && cols > 0;         // the same for all lanes
+            const bool there = src >= 0;
+            look_ahead(u + workers);
             float acc[128];
 #pragma unroll
             for (int i = 0; i < 128; ++i) acc[i] = 0.0f;
             {
-                const Tile t = un.decode(u, P.E, P.N, G::kTileM);
-                const Part pt = part_of(t);
-                const bool active = pt.warp_rows > 0 && pt.cols > 0;         // the same for all lanes
-                const int src = active && lane < pt.warp_rows ? source_row(P, pt.row0 + lane) : -1;
-                const float* xs = P.x_scale + (src >= 0 ? src * P.ld_x_scale : 0);
-                const float* ws = P.w_scale + (static_cast<int64_t>(t.e) * nb + pt.n0 / kFp8Block) * un.kb_all;
-                const int kb1 = t.kb1;
-                // Scales arrive long before they are needed and wait in registers, the row's four at a time.  A row's scales
-                // lie together and a warp's rows do not: 32 lines per load, which the load unit takes one by one while the
-                // barriers of the other warps queue behind it, so the loads are as few and as wide as alignment allows.
-                const auto load_xs = [&](int kb) {             // the aligned group of four that holds block kb
-                    float4 v = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                    const int at = kb & ~3;
-                    if (!active || kb >= kb1) return v;
-                    if (P.xs_vec) return __ldg(reinterpret_cast<const float4*>(xs + at));
-                    v.x = __ldg(xs + at);
-                    if (at + 1 < un.kb_all) v.y = __ldg(xs + at + 1);
-                    if (at + 2 < un.kb_all) v.z = __ldg(xs + at + 2);
-                    if (at + 3 < un.kb_all) v.w = __ldg(xs + at + 3);
-                    return v;
-                };
-                int kb = t.kb0;
-                float4 xs_now = load_xs(kb), xs_next = load_xs((kb & ~3) + 4);
-                float ws_now = active ? __ldg(ws + kb) : 0.0f;
-                for (; kb < kb1; ++kb) {
-                    const float f = ((kb & 2) ? ((kb & 1) ? xs_now.w : xs_now.z) : ((kb & 1) ? xs_now.y : xs_now.x)) * ws_now;
-                    if (active && kb + 1 < kb1) ws_now = __ldg(ws + kb + 1);
-                    if ((kb & 3) == 3) {
-                        xs_now = xs_next;
-                        xs_next = load_xs(kb + 5);
+                for (int c0 = t.kb0; c0 < t.kb1; c0 += 8) {
+                    copy_async_wait();
+                    __syncwarp();
+                    const float* sc = scale_buf + half * kScaleHalf;
+                    half ^= 1;
+                    if (c0 + 8 < t.kb1) {
+                        load_scales(t, src, c0 + 8, half);
+                    } else if (u + workers < un.total) {
+                        src = next_source();
+                        load_scales(next, src, next.kb0, half);
                     }
-                    const int b = n++ & 1;
-                    named_sync(kBarFull + 2 * b + wg, kFullThreads);
-                    tc_fence_after_sync();
-                    if (active) {
-                        const uint32_t at = tmem_mine + b * kTileN;
-                        uint32_t p[32];
+                    const int blocks = min(8, t.kb1 - c0);
+                    for (int i = 0; i < blocks; ++i) {
+                        const float f = sc[lane * kScalePitch + i] * sc[32 * kScalePitch + i];
+                        const int b = n++ & 1;
+                        named_sync(kBarFull + 2 * b + wg, kFullThreads);
+                        tc_fence_after_sync();
+                        if (active) {
+                            const uint32_t at = tmem_mine + b * kTileN;
+                            const float2 f2 = make_float2(f, f);
+                            uint32_t p[2][16];
+                            tmem_ld_16(at, p[0]);
 #pragma unroll
-                        for (int c = 0; c < 4; ++c) {
-                            tmem_ld_32(at + 32 * c, p);
-                            tmem_ld_wait();
-                            if (c == 3) {
-                                tc_fence_before_sync();
-                                named_arrive(kBarEmpty + b, kEmptyThreads);
+                            for (int c = 0; c < 8; ++c) {          // 16 columns on their way while 16 are added
+                                tmem_ld_wait();
+                                if (c < 7) {
+                                    tmem_ld_16(at + 16 * (c + 1), p[(c + 1) & 1]);
+                                } else {
+                                    tc_fence_before_sync();
+                                    named_arrive(kBarEmpty + b, kEmptyThreads);
+                                }
+#pragma unroll
+                                for (int j = 0; j < 16; j += 2) {      // packed: 0.91 additions per cycle and lane, 0.72 one by one
+                                    const float2 r = __ffma2_rn(make_float2(__uint_as_float(p[c & 1][j]), __uint_as_float(p[c & 1][j + 1])),
+                                                                f2, make_float2(acc[c * 16 + j], acc[c * 16 + j + 1]));
+                                    acc[c * 16 + j] = r.x;
+                                    acc[c * 16 + j + 1] = r.y;
+                                }
                             }
-#pragma unroll
-                            for (int i = 0; i < 32; ++i) acc[c * 32 + i] = fmaf(__uint_as_float(p[i]), f, acc[c * 32 + i]);
+                        } else {
+                            named_arrive(kBarEmpty + b, kEmptyThreads);
                         }
-                    } else {
-                        named_arrive(kBarEmpty + b, kEmptyThreads);
                     }
                 }
             }
             // (after a wait that gave up what follows stores numbers that mean nothing, to the places they belong to)
-            int again = u;
-            asm volatile("" : "+r"(again));
-            const Tile t = un.decode(again, P.E, P.N, G::kTileM);
-            const Part pt = part_of(t);
-            const int row0 = pt.row0, warp_rows = pt.warp_rows, n0 = pt.n0, cols = pt.cols;
-            const bool active = warp_rows > 0 && cols > 0, mine = active && lane < warp_rows;
-            const int src = mine ? source_row(P, row0 + lane) : -1;
-
             if (un.splits > 1) {
                 // leave the sums; the part that comes last collects all of them in the order of K.  Every warp keeps its own
                 // counter: nothing here waits for another warp.
@@ -485,7 +543,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
                 __syncwarp();
                 int arrived = 0;
                 if (lane == 0) {
-                    int32_t* ticket = P.tickets + (static_cast<int64_t>(t.tile) * 2 + rank) * 8 + (warp - 4);
+                    int32_t* ticket = P.tickets + (static_cast<int64_t>(u / un.splits) * 2 + rank) * 8 + (warp - 4);
                     arrived = atomicAdd(ticket, 1);
                     if (arrived == un.splits - 1) *ticket = 0;
                     __threadfence();
@@ -493,7 +551,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
                 if (__shfl_sync(0xffffffffu, arrived, 0) != un.splits - 1) continue;
 #pragma unroll
                 for (int i = 0; i < 128; ++i) acc[i] = 0.0f;
-                const float4* part = mine_at - static_cast<size_t>(t.split) * unit_float4;
+                const float4* part = mine_at - static_cast<size_t>(u % un.splits) * unit_float4;
                 for (int s = 0; s < un.splits; ++s) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
@@ -509,22 +567,37 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
             if (!active) continue;
 
             float (&v)[128] = acc;
-            if (src < 0) {                       // no such row: zeros, whatever the gathered stand-in held
+            if (!there) {                        // no such row: zeros, whatever the gathered stand-in held
 #pragma unroll
                 for (int i = 0; i < 128; ++i) v[i] = 0.0f;
             }
             if (P.bias != nullptr) {
                 const float* bias = P.bias + static_cast<int64_t>(t.e) * P.N + n0;
+                if (P.bias_vec && cols == kFp8Block) {
 #pragma unroll
-                for (int i = 0; i < 128; ++i)
-                    if (i < cols) v[i] += __ldg(bias + i);
+                    for (int i = 0; i < 32; ++i) {
+                        const float4 w = __ldg(reinterpret_cast<const float4*>(bias) + i);
+                        v[4 * i] += w.x;
+                        v[4 * i + 1] += w.y;
+                        v[4 * i + 2] += w.z;
+                        v[4 * i + 3] += w.w;
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < 128; ++i)
+                        if (i < cols) v[i] += __ldg(bias + i);
+                }
             }
             if (P.act == MONDE_ACT_RELU) {
 #pragma unroll
                 for (int i = 0; i < 128; ++i) v[i] = max_nan(v[i], 0.0f);
             } else if (P.act == MONDE_ACT_GELU_ERF) {
 #pragma unroll
-                for (int i = 0; i < 128; ++i) v[i] = apply_act(v[i], MONDE_ACT_GELU_ERF);
+                for (int i = 0; i < 128; i += 2) {
+                    const float2 g = gelu2(make_float2(v[i], v[i + 1]));
+                    v[i] = g.x;
+                    v[i + 1] = g.y;
+                }
             }
             if (P.out_dtype == MONDE_BF16) {
                 store_rows<2>(stage_out, static_cast<uint8_t*>(P.out) + (row0 * P.ld_out + n0) * 2, P.ld_out * 2, warp_rows,
@@ -546,7 +619,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
                         if (i < cols) amax = max_nan(amax, fabsf(v[i]));
                 }
                 const float s = block_scale(amax), inv = __fdiv_rn(1.0f, s);
-                if (mine) P.out_scale[(row0 + lane) * P.ld_out_scale + n0 / kFp8Block] = s;
+                if (lane < warp_rows) P.out_scale[(row0 + lane) * P.ld_out_scale + n0 / kFp8Block] = s;
                 store_rows<1>(stage_out, static_cast<uint8_t*>(P.out) + row0 * P.ld_out + n0, P.ld_out, warp_rows, cols,
                               P.out_vec, lane, [&](int i) {
                                   return pack_e4m3(v[4 * i] * inv, v[4 * i + 1] * inv, v[4 * i + 2] * inv, v[4 * i + 3] * inv);
@@ -668,8 +741,8 @@ int matmul(const monde_matmul_problem* p, const void* x, const float* x_scale, c
     P.row_ids = row_ids;
     P.out = out;
     P.out_scale = out_scale;
-    P.xs_vec = aligned(x_scale, 16) && p->ld_x_scale % 4 == 0 && ((p->K + kFp8Block - 1) / kFp8Block) % 4 == 0;
-    P.out_vec = aligned(out, 16) && (p->ld_out * ob) % 16 == 0;
+    P.out_vec = aligned(out, 32) && (p->ld_out * ob) % 32 == 0;
+    P.bias_vec = aligned(bias, 16) && p->N % 4 == 0;
     P.status = reinterpret_cast<int32_t*>(base + WsLayout::kStatus);
     P.tickets = reinterpret_cast<int32_t*>(base + WsLayout::kPartDone);
     P.partials = reinterpret_cast<float4*>(base + WsLayout::kHidden);
