@@ -16,7 +16,7 @@
 
 #include <type_traits>
 
-#include "fp8.cuh"
+#include "fp8_matmul.cuh"
 #include "sm100.cuh"
 
 namespace monde {
@@ -24,24 +24,6 @@ namespace monde {
 namespace {
 
 using namespace sm100;
-
-struct MatmulParams {
-    int rows, N, K, E, src_rows, row_div, act, out_dtype;
-    int64_t ld_x_scale, ld_out, ld_out_scale;
-    const float* x_scale;
-    const float* w_scale;
-    const float* bias;
-    const int32_t* offsets;     // null: one matrix, all rows
-    const int32_t* row_ids;     // null: position r reads row r
-    void* out;
-    float* out_scale;
-    int out_vec;                // rows of `out` start on 32-byte boundaries
-    int bias_vec;               // rows of `bias` start on 16-byte boundaries
-    int32_t* status;            // {status, site}
-    int32_t* tickets;           // [tile][CTA of the pair][epilogue warp]: parts of a K-split tile that have finished (zero between calls)
-    float4* partials;           // [unit][CTA of the pair][column half][32][128 threads]
-    unsigned long long wait_ns;
-};
 
 // Boxes of the row operand: as many rows as a small tile needs (a box row that is not needed still costs its trip through
 // L2); with row ids one row, gathered four at a time.
@@ -65,6 +47,7 @@ constexpr size_t kUnitPartialBytes = size_t(kRowsPerCta) * kTileN * 4;
 constexpr int kStageWarpBytes = 32 * 16;                            // output rows that cannot go out straight
 constexpr int kScalePitch = 9, kScaleHalf = 33 * kScalePitch;        // scales of eight K blocks: 32 rows and the weights'
 constexpr int kScaleWarpBytes = 2 * kScaleHalf * 4;
+constexpr int kCopyRowsPerExpert = 32;   // from here on rows picked by id are copied first
 constexpr int kRowGroup = 8;           // row tiles that go together through the columns
 
 
@@ -147,14 +130,6 @@ template <bool kPair> struct Geometry {
     static constexpr int kSmem = 1024 + kStages * kStageBytes + 8 * (kStageWarpBytes + kScaleWarpBytes) + kBars * 8 + 64 + static_cast<int>(sizeof(Units));
 };
 
-// The row of x that output row r reads, in two steps so that the load can be issued long before its answer is needed.
-__device__ __forceinline__ int load_row_id(const MatmulParams& P, int r) { return P.row_ids != nullptr ? P.row_ids[r] : r; }
-__device__ __forceinline__ int source_row(const MatmulParams& P, int id) {      // -1: no such row
-    if (P.row_ids == nullptr) return id;
-    const int s = id < 0 ? -1 : id / P.row_div;
-    return s < P.src_rows ? s : -1;
-}
-
 // 128 columns of 32 rows, a row per lane, to global memory; `word(i)`: 32-bit word i of this lane's row.  Whole tiles whose
 // rows start on 32-byte boundaries go out straight from registers, a sector per lane and store; others 16 bytes of each row
 // at a time through shared memory, element by element.
@@ -209,7 +184,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
     const auto peer_empty = [&](int b) { return bar0 + 8u * (2 * G::kStages + 2 + b); };
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const bool gather = P.row_ids != nullptr;
+    const bool gather = P.tma_gather != 0;
     pdl_launch_dependents();
     if (tid == 0) {
         *abort_flag = 0;
@@ -265,7 +240,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
             un.n_tiles = (P.N + kTileN - 1) / kTileN;
             un.kb_all = (P.K + kFp8Block - 1) / kFp8Block;
             const int tiles = prefix[P.E] * un.n_tiles;
-            un.splits = choose_splits(tiles, workers, un.kb_all);
+            un.splits = P.may_split ? choose_splits(tiles, workers, un.kb_all) : 1;
             un.total = tiles * un.splits;
         }
     }
@@ -643,6 +618,20 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
     }
 }
 
+// Rows picked by id, copied side by side (a row that is not there becomes zeros): 16 bytes a thread.
+__global__ void __launch_bounds__(256) gather_rows_kernel(const MatmulParams P, uint8_t* __restrict__ out) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const int per_row = P.K / 16;
+    const int64_t i = static_cast<int64_t>(blockIdx.x) * blockDim.x + threadIdx.x;
+    const int64_t row = i / per_row;
+    if (row >= P.rows) return;
+    const int c = static_cast<int>(i - row * per_row) * 16;
+    const int s = source_row(P, load_row_id(P, static_cast<int>(row)));
+    *reinterpret_cast<uint4*>(out + row * P.K + c) =
+        s >= 0 ? *reinterpret_cast<const uint4*>(P.x + s * P.ld_x + c) : make_uint4(0, 0, 0, 0);
+}
+
 // ---- host side ---------------------------------------------------------------------------------------------------------
 
 using EncodeTiledFn = CUresult (*)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
@@ -733,7 +722,7 @@ int matmul(const monde_matmul_problem* p, const void* x, const float* x_scale, c
     MatmulParams P;
     P.rows = p->rows; P.N = p->N; P.K = p->K; P.E = p->E;
     P.src_rows = p->src_rows; P.row_div = p->row_div; P.act = p->act; P.out_dtype = p->out_dtype;
-    P.ld_x_scale = p->ld_x_scale; P.ld_out = p->ld_out; P.ld_out_scale = p->ld_out_scale;
+    P.ld_x = p->ld_x; P.x = static_cast<const uint8_t*>(x); P.ld_x_scale = p->ld_x_scale; P.ld_out = p->ld_out; P.ld_out_scale = p->ld_out_scale;
     P.x_scale = x_scale;
     P.w_scale = w_scale;
     P.bias = bias;
@@ -747,14 +736,38 @@ int matmul(const monde_matmul_problem* p, const void* x, const float* x_scale, c
     P.tickets = reinterpret_cast<int32_t*>(base + WsLayout::kPartDone);
     P.partials = reinterpret_cast<float4*>(base + WsLayout::kHidden);
     P.wait_ns = diag.wait_limit_ns;
+    cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (p->rows <= kMatvecRows) return launch_matvec_fp8(P, w, s);
+    // Rows picked by id: TMA's gather brings four rows in some 90 cycles, whatever their length, which passes unnoticed behind
+    // the weights of a small tile but not at 128 rows (1.5 us per K block, twice the multiplication).  From 32 rows per expert
+    // on the rows are first copied side by side into the part of the workspace that K-split tiles would use, where there
+    // are too many tiles for a split and the copy fits.  128 experts 1024 -> 4096, gathered and copied: 16 rows each 96 and
+    // 100 us, 32 rows 99 and 102, 64 rows 126 and 116, 128 rows 185 and 134; 32 rows on average with a skewed router
+    // (2048 -> 8192) 450 and 404.
+    const size_t copy_bytes = static_cast<size_t>(p->rows) * p->K;
+    const bool copy_rows = row_ids != nullptr && p->rows >= kCopyRowsPerExpert * p->E &&
+                           p->rows / 128 * col_tiles > kMaxSplitUnits / 2 && copy_bytes <= ws_bytes - WsLayout::kHidden;
+    P.tma_gather = row_ids != nullptr && !copy_rows;
+    P.may_split = !copy_rows;
+    const void* rows_at = x;
+    uint64_t rows_n = p->src_rows, rows_ld = p->ld_x;
+    if (copy_rows) {
+        rows_at = base + WsLayout::kHidden;
+        rows_n = p->rows;
+        rows_ld = p->K;
+        const int64_t threads = static_cast<int64_t>(p->rows) * (p->K / 16);
+        if (launch_pdl(gather_rows_kernel, dim3(static_cast<unsigned>((threads + 255) / 256)), dim3(256), 0, s, P,
+                       reinterpret_cast<uint8_t*>(base) + WsLayout::kHidden) != cudaSuccess)
+            return MONDE_ERR_CUDA;
+        count_launches(1);
+    }
     MatmulMaps M;
     for (int i = 0; i < 3; ++i) {
-        if (!make_map(&M.a[i], x, p->src_rows, p->K, p->ld_x, row_ids != nullptr ? 1 : kRowsPerCta >> i)) return MONDE_ERR_CUDA;
+        if (!make_map(&M.a[i], rows_at, rows_n, p->K, rows_ld, P.tma_gather ? 1 : kRowsPerCta >> i)) return MONDE_ERR_CUDA;
         if (i < 2 && !make_map(&M.w[i], w, static_cast<uint64_t>(p->E) * p->N, p->K, p->K, (pair ? 128 : 256) >> i))
             return MONDE_ERR_CUDA;
     }
     const int sms = current_sm_count();
-    cudaStream_t s = static_cast<cudaStream_t>(stream);
     const cudaError_t err = pair
         ? launch_pdl_cluster(matmul_fp8_kernel<true>, dim3(sms & ~1), dim3(kThreads), Geometry<true>::kSmem, 2, s, M, P)
         : launch_pdl(matmul_fp8_kernel<false>, dim3(sms), dim3(kThreads), Geometry<false>::kSmem, s, M, P);

@@ -1,0 +1,41 @@
+// What the two block-scaled product kernels share: their parameters, and the rows that row ids stand for.
+#pragma once
+
+#include "fp8.cuh"
+
+namespace monde {
+
+struct MatmulParams {
+    int rows, N, K, E, src_rows, row_div, act, out_dtype;
+    int64_t ld_x, ld_x_scale, ld_out, ld_out_scale;
+    const uint8_t* x;
+    const float* x_scale;
+    const float* w_scale;
+    const float* bias;
+    const int32_t* offsets;     // null: one matrix, all rows
+    const int32_t* row_ids;     // null: position r reads row r
+    void* out;
+    float* out_scale;
+    int may_split;              // the workspace's space for parts is free
+    int tma_gather;             // rows of x are picked by id while they are loaded (else: they lie in order)
+    int out_vec;                // rows of `out` start on 32-byte boundaries
+    int bias_vec;               // rows of `bias` start on 16-byte boundaries
+    int32_t* status;            // {status, site}
+    int32_t* tickets;           // [tile][CTA of the pair][epilogue warp]: parts of a K-split tile that have finished (zero between calls)
+    float4* partials;           // [unit][CTA of the pair][column half][32][128 threads]
+    unsigned long long wait_ns;
+};
+
+// The row of x that output row r reads, in two steps so that the load can be issued long before its answer is needed.
+__device__ __forceinline__ int load_row_id(const MatmulParams& P, int r) { return P.row_ids != nullptr ? P.row_ids[r] : r; }
+__device__ __forceinline__ int source_row(const MatmulParams& P, int id) {      // -1: no such row
+    if (P.row_ids == nullptr) return id;
+    const int s = id < 0 ? -1 : id / P.row_div;
+    return s < P.src_rows ? s : -1;
+}
+
+// The product for a few rows in all (fp8_matvec.cu): weights stream through registers, no tensor memory, no workspace.
+constexpr int kMatvecRows = 32;
+int launch_matvec_fp8(const MatmulParams& P, const void* w, cudaStream_t s);
+
+}  // namespace monde
