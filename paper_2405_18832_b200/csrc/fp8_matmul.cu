@@ -14,6 +14,7 @@
 // adds them in the order of K, whoever it is, so results are bit-reproducible and nobody waits.
 #include <cuda.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "fp8_matmul.cuh"
@@ -69,7 +70,7 @@ struct Tile {
 // them spill.
 struct Units {
     int total, splits;              // units; parts per tile
-    int n_tiles, kb_all;            // 256-column tiles of a row tile; K blocks
+    int tile_n, n_tiles, kb_all;    // columns of a tile, tiles of a row tile; K blocks
     uint32_t inverse[kMaxSplit + 1];    // ceil(2^32 / d)
     int prefix[kMaxExperts + 1];    // row tiles of the experts before e
     int first[kMaxExperts + 1];     // first row of expert e
@@ -96,8 +97,8 @@ struct Units {
         const int m = g * kRowGroup + local - n * in_group;
         t.r0 = first[t.e] + m * tile_m;
         t.rows = min(tile_m, first[t.e + 1] - t.r0);
-        t.n0 = n * kTileN;
-        t.cols = min(kTileN, N - t.n0);
+        t.n0 = n * tile_n;
+        t.cols = min(tile_n, N - t.n0);
         t.kb0 = 0;
         t.kb1 = kb_all;
         if (parts > 1) {                     // (K < 2^31, at most 16 parts: no overflow)
@@ -109,15 +110,16 @@ struct Units {
     __device__ __forceinline__ uint32_t small_inverse(int d) const { return inverse[d]; }
 };
 
-// Parts of the K range: as many as shorten the longest CTA's work, counted in K blocks, where a split tile pays about
-// four K blocks for leaving and collecting its parts.
-__device__ __forceinline__ int choose_splits(int tiles, int workers, int kb_all) {
-    int best = 1, best_cost = (tiles + workers - 1) / workers * kb_all;
-    for (int s = 2; s <= kMaxSplit && s <= kb_all && tiles * s <= min(kMaxSplitUnits, 2 * workers); ++s) {
-        const int cost = (tiles * s + workers - 1) / workers * ((kb_all + s - 1) / s + 4);
-        if (cost < best_cost) { best = s; best_cost = cost; }
-    }
-    return best;
+// Parts of the K range: as many as shorten the longest CTA's work, counted in K blocks, where a split tile pays about eight K
+// blocks for leaving its sums and half a block per part for collecting them.  Lane i of a warp weighs i + 1 parts.
+__device__ __forceinline__ int choose_splits(int tiles, int workers, int kb_all, int lane) {
+    const int s = lane + 1;
+    int cost = 0x7fffffff;
+    if (s == 1) cost = (tiles + workers - 1) / workers * kb_all;
+    else if (s <= kMaxSplit && s <= kb_all && tiles * s <= min(kMaxSplitUnits, 2 * workers))
+        cost = (tiles * s + workers - 1) / workers * ((kb_all + s - 1) / s + 8 + s / 2);
+    const int best = __reduce_min_sync(0xffffffffu, cost);
+    return __ffs(__ballot_sync(0xffffffffu, cost == best));      // the fewest among equals
 }
 
 template <bool kPair> struct Geometry {
@@ -236,12 +238,17 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
     if (tid >= 2 && tid <= kMaxSplit) un.inverse[tid] = 0xffffffffu / static_cast<uint32_t>(tid) + 1;
     if (warp == 0) {
         __syncwarp();
+        // half-width tiles where full ones would leave half of the CTAs without any
+        const int row_tiles = prefix[P.E], wide = (P.N + kTileN - 1) / kTileN;
+        const int tile_n = static_cast<int64_t>(row_tiles) * wide * 2 <= workers ? kTileN / 2 : kTileN;
+        const int n_tiles = (P.N + tile_n - 1) / tile_n, kb_all = (P.K + kFp8Block - 1) / kFp8Block;
+        const int splits = P.may_split ? choose_splits(row_tiles * n_tiles, workers, kb_all, lane) : 1;
         if (lane == 0) {
-            un.n_tiles = (P.N + kTileN - 1) / kTileN;
-            un.kb_all = (P.K + kFp8Block - 1) / kFp8Block;
-            const int tiles = prefix[P.E] * un.n_tiles;
-            un.splits = P.may_split ? choose_splits(tiles, workers, un.kb_all) : 1;
-            un.total = tiles * un.splits;
+            un.tile_n = tile_n;
+            un.n_tiles = n_tiles;
+            un.kb_all = kb_all;
+            un.splits = splits;
+            un.total = row_tiles * n_tiles * splits;
         }
     }
     tc_fence_before_sync();
@@ -411,7 +418,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
             p.row0 = t.r0 + static_cast<int>(rank) * kRowsPerCta + quarter * 32;       // of the warp
             p.warp_rows = min(max(rows_of(t, rank) - quarter * 32, 0), 32);
             p.n0 = t.n0 + wg * (kTileN / 2);
-            p.cols = min(max(P.N - p.n0, 0), kTileN / 2);
+            p.cols = min(max(t.cols - wg * (kTileN / 2), 0), kTileN / 2);
             p.e = t.e;
             p.kb0 = t.kb0;
             p.kb1 = t.kb1;
@@ -737,7 +744,13 @@ int matmul(const monde_matmul_problem* p, const void* x, const float* x_scale, c
     P.partials = reinterpret_cast<float4*>(base + WsLayout::kHidden);
     P.wait_ns = diag.wait_limit_ns;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (p->rows <= kMatvecRows) return launch_matvec_fp8(P, w, s);
+    // A few rows: the kernel without tensor memory starts sooner and streams slower.  It is taken up to 32 MB of weights, where
+    // eight rows more cost it as much as the weights again, and an e4m3 output as well.  (us, other kernel second: one row
+    // 4096 x 4096 8.6 and 21.1, 8192 x 8192 20.5 and 24.3; 4 of 128 experts 1024 -> 4096 9.2 and 11; 27 of them 38.6 and 27.9,
+    // with an e4m3 output 74.9 and 29.5.)
+    const int64_t matrices = grouped ? std::min(p->E, p->rows) : 1;
+    const int64_t passes = (grouped || p->rows <= 8 ? 1 : p->rows <= 16 ? 2 : 4) * (p->out_dtype == MONDE_E4M3 ? 2 : 1);
+    if (p->rows <= kMatvecRows && matrices * p->N * p->K * passes <= (32 << 20)) return launch_matvec_fp8(P, w, s);
     // Rows picked by id: TMA's gather brings four rows in some 90 cycles, whatever their length, which passes unnoticed behind
     // the weights of a small tile but not at 128 rows (1.5 us per K block, twice the multiplication).  From 32 rows per expert
     // on the rows are first copied side by side into the part of the workspace that K-split tiles would use, where there
