@@ -52,7 +52,7 @@ constexpr int kCopyRowsPerExpert = 32;   // from here on rows picked by id are c
 constexpr int kRowGroup = 8;           // row tiles that go together through the columns
 
 
-enum WaitSite { kSiteLoad = 21, kSiteMmaOperands = 22, kSiteMmaAcc = 23, kSiteEpilogue = 24 };
+enum WaitSite { kSiteLoad = 21, kSiteMmaOperands = 22, kSiteEpilogue = 23 };
 
 __device__ __forceinline__ void give_up(int32_t* status, volatile int* abort_flag, int site) {
     *abort_flag = 1;
@@ -122,31 +122,37 @@ __device__ __forceinline__ int choose_splits(int tiles, int workers, int kb_all,
     return __ffs(__ballot_sync(0xffffffffu, cost == best));      // the fewest among equals
 }
 
-template <bool kPair> struct Geometry {
-    static constexpr int kTileM = kPair ? 256 : 128;              // rows of a tile (a pair: 128 in each CTA)
-    static constexpr int kBBytes = (kPair ? 128 : 256) * kRowBytes;   // weight rows a CTA loads
-    static constexpr int kStageBytes = kABytes + kBBytes;
-    static constexpr int kStages = kPair ? 6 : 4;
-    static_assert(kStages % 2 == 0, "the MMA warps take every other stage");
-    static constexpr int kBars = 2 * kStages + 4;
-    static constexpr int kSmem = 1024 + kStages * kStageBytes + 8 * (kStageWarpBytes + kScaleWarpBytes) + kBars * 8 + 64 + static_cast<int>(sizeof(Units));
-};
+constexpr int kBBytes = kTileN * kRowBytes;                           // weight rows of a stage
+constexpr int kStageBytes = kABytes + kBBytes;
+constexpr int kStages = 4;
+static_assert(kStages % 2 == 0, "the MMA warps take every other stage");
+constexpr int kBars = 2 * kStages + 2;
+constexpr int kSmemBytes = 1024 + kStages * kStageBytes + 8 * (kStageWarpBytes + kScaleWarpBytes) + kBars * 8 + 64 +
+                           static_cast<int>(sizeof(Units));
+static_assert(kSmemBytes <= 227 * 1024, "shared memory of a CTA");
 
-// 128 columns of 32 rows, a row per lane, to global memory; `word(i)`: 32-bit word i of this lane's row.  Whole tiles whose
-// rows start on 32-byte boundaries go out straight from registers, a sector per lane and store; others 16 bytes of each row
-// at a time through shared memory, element by element.
+// Up to 128 columns of 32 rows, a row per lane, to global memory; `word(i)`: 32-bit word i of this lane's row.  Rows that start
+// on 32-byte boundaries go out straight from registers, a sector per lane and store; others 16 bytes of each row at a time
+// through shared memory, element by element.
 template <int kEsize, typename F>
 __device__ __forceinline__ void store_rows(uint8_t* stage, uint8_t* out_row0, int64_t ld_bytes, int rows, int cols,
                                            bool vec, int lane, F word) {
-    if (vec && cols == kFp8Block) {
-        if (lane < rows) {
-            uint8_t* dst = out_row0 + lane * ld_bytes;
+    const int bytes = cols * kEsize;
+    if (vec && bytes % 32 == 0) {
+        if (lane >= rows) return;
+        uint8_t* dst = out_row0 + lane * ld_bytes;
+        const auto put = [&](int p) {
+            const uint32_t w[8] = {word(p * 8), word(p * 8 + 1), word(p * 8 + 2), word(p * 8 + 3),
+                                   word(p * 8 + 4), word(p * 8 + 5), word(p * 8 + 6), word(p * 8 + 7)};
+            store_32(dst + p * 32, w);
+        };
+        if (cols == kFp8Block) {
 #pragma unroll
-            for (int p = 0; p < kEsize * 4; ++p) {
-                const uint32_t w[8] = {word(p * 8), word(p * 8 + 1), word(p * 8 + 2), word(p * 8 + 3),
-                                       word(p * 8 + 4), word(p * 8 + 5), word(p * 8 + 6), word(p * 8 + 7)};
-                store_32(dst + p * 32, w);
-            }
+            for (int p = 0; p < kEsize * 4; ++p) put(p);
+        } else {
+#pragma unroll
+            for (int p = 0; p < kEsize * 4; ++p)
+                if (p * 32 < bytes) put(p);
         }
         return;
     }
@@ -167,43 +173,39 @@ __device__ __forceinline__ void store_rows(uint8_t* stage, uint8_t* out_row0, in
     }
 }
 
-template <bool kPair>
 __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_constant__ MatmulMaps M, const MatmulParams P) {
-    using G = Geometry<kPair>;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
-    uint8_t* staging = smem + G::kStages * G::kStageBytes;
+    uint8_t* staging = smem + kStages * kStageBytes;
     uint64_t* bars = reinterpret_cast<uint64_t*>(staging + 8 * (kStageWarpBytes + kScaleWarpBytes));
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + G::kBars);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + kBars);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     Units& un = *reinterpret_cast<Units*>(tmem_slot + 16);
     int* const prefix = un.prefix;
     int* const first = un.first;
     const uint32_t bar0 = smem_u32(bars);
     const auto full = [&](int s) { return bar0 + 8u * s; };
-    const auto empty = [&](int s) { return bar0 + 8u * (G::kStages + s); };
-    const auto acc_full = [&](int b) { return bar0 + 8u * (2 * G::kStages + b); };
-    const auto peer_empty = [&](int b) { return bar0 + 8u * (2 * G::kStages + 2 + b); };
+    const auto empty = [&](int s) { return bar0 + 8u * (kStages + s); };
+    const auto acc_full = [&](int b) { return bar0 + 8u * (2 * kStages + b); };
 
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const bool gather = P.tma_gather != 0;
     pdl_launch_dependents();
     if (tid == 0) {
         *abort_flag = 0;
-        for (int s = 0; s < G::kStages; ++s) {
-            mbar_init(full(s), 1);      // the weight producer's expect_tx (of the leader CTA)
+        for (int s = 0; s < kStages; ++s) {
+            mbar_init(full(s), 1);      // the loading warp's expect_tx
             mbar_init(empty(s), 1);     // one commit
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(acc_full(b), 1);                    // one commit
-            mbar_init(peer_empty(b), 1);                  // the other CTA of a pair has read its half
         }
         fence_barrier_init();
         for (int i = 0; i < 3; ++i) prefetch_tensormap(&M.a[i]);
         for (int i = 0; i < 2; ++i) prefetch_tensormap(&M.w[i]);
     } else if (warp == 1) {
-        if (kPair) { tmem_alloc_pair(smem_u32(tmem_slot), 512); tmem_relinquish_pair(); }
-        else { tmem_alloc(smem_u32(tmem_slot), 512); tmem_relinquish(); }
+        tmem_alloc(smem_u32(tmem_slot), 512);
+        tmem_relinquish();
     }
     pdl_wait();
 
@@ -216,7 +218,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const int e = lane * 8 + i;
-            v[i] = e < P.E ? (max(first[e + 1] - first[e], 0) + G::kTileM - 1) / G::kTileM : 0;
+            v[i] = e < P.E ? (max(first[e + 1] - first[e], 0) + kRowsPerCta - 1) / kRowsPerCta : 0;
             sum += v[i];
         }
         int inc = sum;
@@ -233,8 +235,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
             if (lane * 8 + i < P.E) prefix[lane * 8 + i + 1] = run;
         }
     }
-    const int workers = kPair ? static_cast<int>(gridDim.x) / 2 : static_cast<int>(gridDim.x);
-    const int worker = kPair ? static_cast<int>(blockIdx.x) / 2 : static_cast<int>(blockIdx.x);
+    const int workers = gridDim.x, worker = blockIdx.x;
     if (tid >= 2 && tid <= kMaxSplit) un.inverse[tid] = 0xffffffffu / static_cast<uint32_t>(tid) + 1;
     if (warp == 0) {
         __syncwarp();
@@ -253,18 +254,12 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
     }
     tc_fence_before_sync();
     __syncthreads();
-    if (kPair) cluster_sync_all();
     tc_fence_after_sync();
     const uint32_t tmem_base = *tmem_slot;
-    const uint32_t rank = kPair ? cluster_ctarank() : 0u;
-    const uint32_t bar0_leader = kPair ? map_to_cta(bar0, 0) : bar0;
     const uint32_t stages_u32 = smem_u32(smem);
 
-    // Rows of the tile that CTA `r` of the pair holds, and the bytes its row loads bring.
-    const auto rows_of = [&](const Tile& t, uint32_t r) { return min(max(t.rows - static_cast<int>(r) * kRowsPerCta, 0), kRowsPerCta); };
-    const auto a_bytes_of = [&](int rows) {
-        if (gather) return (rows + 3) / 4 * 4 * kRowBytes;
-        return rows == 0 ? 0 : (rows <= 32 ? 32 : (rows <= 64 ? 64 : 128)) * kRowBytes;
+    const auto a_bytes_of = [&](int rows) {          // what the row loads of a K block bring
+        return gather ? (rows + 3) / 4 * 4 * kRowBytes : (rows <= 32 ? 32 : (rows <= 64 ? 64 : 128)) * kRowBytes;
     };
 
     // Whole warps wait, and one lane of them issues: a lane that loops alone while the others sit at the end of the branch
@@ -282,7 +277,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
             if (worker < un.total) n = static_cast<uint32_t>((un.total - 1 - worker) / workers + 1) * un.kb_all;
         } else {
             for (int u = worker; u < un.total; u += workers) {
-                const Tile t = un.decode(u, lane, P.E, P.N, G::kTileM);
+                const Tile t = un.decode(u, lane, P.E, P.N, kRowsPerCta);
                 n += t.kb1 - t.kb0;
             }
         }
@@ -302,8 +297,8 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
             int4 ids = make_int4(0, 0, 0, 0);
             const auto look_ahead = [&](int u) {
                 if (u >= un.total) return;
-                next = un.decode(u, lane, P.E, P.N, G::kTileM);
-                const int rows = rows_of(next, rank), r = next.r0 + static_cast<int>(rank) * kRowsPerCta + 4 * lane;
+                next = un.decode(u, lane, P.E, P.N, kRowsPerCta);
+                const int rows = next.rows, r = next.r0 + 4 * lane;
                 if (gather && 4 * lane < rows)
                     ids = make_int4(P.row_ids[r], 4 * lane + 1 < rows ? P.row_ids[r + 1] : 0,
                                     4 * lane + 2 < rows ? P.row_ids[r + 2] : 0, 4 * lane + 3 < rows ? P.row_ids[r + 3] : 0);
@@ -311,15 +306,12 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
             look_ahead(worker);
             for (int u = worker; ok && u < un.total; u += workers) {
                 const Tile t = next;
-                const int rows = rows_of(t, rank);
+                const int rows = t.rows;
                 const bool half = t.cols <= kTileN / 2;
                 const CUtensorMap* mw = &M.w[half];
-                const int b_rows = (half ? kTileN / 2 : kTileN) / (kPair ? 2 : 1);
                 const CUtensorMap* ma = &M.a[rows <= 32 ? 2 : (rows <= 64 ? 1 : 0)];
-                const uint32_t bytes = a_bytes_of(rows_of(t, 0)) + (kPair ? a_bytes_of(rows_of(t, 1)) : 0) +
-                                       (kPair ? 2 : 1) * b_rows * kRowBytes;
-                const int w_row = t.e * P.N + t.n0 + static_cast<int>(rank) * b_rows;
-                const int a_row = t.r0 + static_cast<int>(rank) * kRowsPerCta;
+                const uint32_t bytes = a_bytes_of(rows) + (half ? kBBytes / 2 : kBBytes);
+                const int w_row = t.e * P.N + t.n0;
                 const bool gathers = gather && 4 * lane < rows;
                 int4 src = make_int4(0, 0, 0, 0);       // a row that is not there reads row 0, and is not used
                 if (gathers)
@@ -328,26 +320,18 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
                 look_ahead(u + workers);
                 for (int kb = t.kb0; kb < t.kb1; ++kb) {
                     if (!wait_all(empty(stage), phase ^ 1, kSiteLoad)) { ok = false; break; }
-                    const uint32_t dst = stages_u32 + stage * G::kStageBytes, bar = bar0_leader + 8u * stage;
+                    const uint32_t dst = stages_u32 + stage * kStageBytes;
                     if (lane == 0) {
-                        if (rank == 0) mbar_arrive_expect_tx(full(stage), bytes);
-                        if (kPair) {
-                            tma_load_2d_pair(dst + kABytes, mw, bar, kb * kRowBytes, w_row, pol_w);
-                            if (!gather && rows > 0) tma_load_2d_pair(dst, ma, bar, kb * kRowBytes, a_row, pol_a);
-                        } else {
-                            tma_load_2d(dst + kABytes, mw, bar, kb * kRowBytes, w_row, pol_w);
-                            if (!gather) tma_load_2d(dst, ma, bar, kb * kRowBytes, a_row, pol_a);
-                        }
+                        mbar_arrive_expect_tx(full(stage), bytes);
+                        tma_load_2d(dst + kABytes, mw, full(stage), kb * kRowBytes, w_row, pol_w);
+                        if (!gather) tma_load_2d(dst, ma, full(stage), kb * kRowBytes, t.r0, pol_a);
                     }
-                    if (gathers) {
-                        if (kPair) tma_gather4_pair(dst + lane * 4 * kRowBytes, &M.a[0], bar, kb * kRowBytes, src, pol_a);
-                        else tma_gather4(dst + lane * 4 * kRowBytes, &M.a[0], bar, kb * kRowBytes, src, pol_a);
-                    }
+                    if (gathers) tma_gather4(dst + lane * 4 * kRowBytes, &M.a[0], full(stage), kb * kRowBytes, src, pol_a);
                     __syncwarp();
-                    if (++stage == G::kStages) { stage = 0; phase ^= 1; }
+                    if (++stage == kStages) { stage = 0; phase ^= 1; }
                 }
             }
-        } else if ((warp == 1 || warp == 2) && rank == 0) {
+        } else if (warp <= 2) {
             // ---- MMA issue: two warps take turns, one accumulator each -------------------------------------------------
             // Issuing a block's four MMAs takes the warp as long as the tensor core takes to run them, and its waits add some
             // 350 cycles: with one warp the tensor core stood still for those.
@@ -355,43 +339,33 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
             int stage = b;
             uint32_t phase = 0, n = 0;         // n: K blocks so far; block n uses accumulator n & 1
             bool ok = true;
-            Tile t = un.decode(worker, lane, P.E, P.N, G::kTileM);
+            Tile t = un.decode(worker, lane, P.E, P.N, kRowsPerCta);
             for (int u = worker; u < un.total; u += workers) {
-                const uint32_t idesc = idesc_e4m3(G::kTileM, t.cols <= kTileN / 2 ? kTileN / 2 : kTileN);
+                const uint32_t idesc = idesc_e4m3(kRowsPerCta, t.cols <= kTileN / 2 ? kTileN / 2 : kTileN);
                 const int blocks = t.kb1 - t.kb0;
                 // (the next tile is found while this one's first blocks are multiplied)
                 for (int i = 0; i < blocks; ++i, ++n) {
-                    if (i == min(2, blocks - 1) && u + workers < un.total) t = un.decode(u + workers, lane, P.E, P.N, G::kTileM);
+                    if (i == min(2, blocks - 1) && u + workers < un.total) t = un.decode(u + workers, lane, P.E, P.N, kRowsPerCta);
                     if ((n & 1) != b) continue;
                     // operands first: that wait passes while the blocks before are still being multiplied
                     ok = ok && wait_all(full(stage), phase, kSiteMmaOperands);
-                    if (n >= 2) {
-                        named_sync(kBarEmpty + b, kEmptyThreads);
-                        if (kPair) ok = ok && wait_all(peer_empty(b), ((n >> 1) - 1) & 1, kSiteMmaAcc);
-                    }
+                    if (n >= 2) named_sync(kBarEmpty + b, kEmptyThreads);
                     tc_fence_after_sync();
                     if (ok && lane == 0) {
-                        const uint64_t a = smem_desc_sw128(stages_u32 + stage * G::kStageBytes);
-                        const uint64_t w = smem_desc_sw128(stages_u32 + stage * G::kStageBytes + kABytes);
+                        const uint64_t a = smem_desc_sw128(stages_u32 + stage * kStageBytes);
+                        const uint64_t w = smem_desc_sw128(stages_u32 + stage * kStageBytes + kABytes);
 #pragma unroll
                         for (int k = 0; k < 4; ++k)          // 32 of the block's 128 columns each
-                            umma_f8<kPair>(tmem_base + b * kTileN, a + 2 * k, w + 2 * k, idesc, k != 0);
-                        if (kPair) { umma_commit_pair(acc_full(b)); umma_commit_pair(empty(stage)); }
-                        else { umma_commit(acc_full(b)); umma_commit(empty(stage)); }
+                            umma_f8(tmem_base + b * kTileN, a + 2 * k, w + 2 * k, idesc, k != 0);
+                        umma_commit(acc_full(b));
+                        umma_commit(empty(stage));
                     }
                     __syncwarp();
-                    if ((stage += 2) >= G::kStages) { stage -= G::kStages; phase ^= 1; }
+                    if ((stage += 2) >= kStages) { stage -= kStages; phase ^= 1; }
                 }
             }
             if (n > static_cast<uint32_t>(b)) named_sync(kBarEmpty + b, kEmptyThreads);      // the last block's
-        } else if (warp == 1) {
-            // ---- the other CTA of a pair: tells the leader which accumulators its epilogue has read ----------------
-            const uint32_t total = count_blocks();
-            for (uint32_t n = 0; n < total; ++n) {
-                named_sync(kBarEmpty + (n & 1), kEmptyThreads);
-                if (lane == 0) mbar_arrive_relaxed_cluster(bar0_leader + 8u * (2 * G::kStages + 2 + (n & 1)));
-            }
-        } else if (warp == 3) {
+        } else {
             // ---- finished accumulators: this warp alone polls their barriers and wakes the epilogue's ----------------
             const uint32_t total = count_blocks();
             for (uint32_t n = 0; n < total; ++n) {
@@ -415,8 +389,8 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
         struct Part { int row0, warp_rows, n0, cols, e, kb0, kb1; };
         const auto part_of = [&](const Tile& t) {
             Part p;
-            p.row0 = t.r0 + static_cast<int>(rank) * kRowsPerCta + quarter * 32;       // of the warp
-            p.warp_rows = min(max(rows_of(t, rank) - quarter * 32, 0), 32);
+            p.row0 = t.r0 + quarter * 32;            // of the warp
+            p.warp_rows = min(max(t.rows - quarter * 32, 0), 32);
             p.n0 = t.n0 + wg * (kTileN / 2);
             p.cols = min(max(t.cols - wg * (kTileN / 2), 0), kTileN / 2);
             p.e = t.e;
@@ -446,7 +420,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
         int next_id = 0;
         const auto look_ahead = [&](int u) {
             if (u >= un.total) return;
-            next = part_of(un.decode(u, lane, P.E, P.N, G::kTileM));
+            next = part_of(un.decode(u, lane, P.E, P.N, kRowsPerCta));
             if (next.cols > 0 && lane < next.warp_rows) next_id = load_row_id(P, next.row0 + lane);
         };
         const auto next_source = [&]() { return next.cols > 0 && lane < next.warp_rows ? source_row(P, next_id) : -1; };
@@ -514,9 +488,8 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
                 // leave the sums; the part that comes last collects all of them in the order of K.  Every warp keeps its own
                 // counter: nothing here waits for another warp.
                 if (!active) continue;
-                const size_t unit_float4 = kUnitPartialBytes / 16 * (kPair ? 2 : 1);
-                float4* mine_at = P.partials + static_cast<size_t>(u) * unit_float4 +
-                                  (static_cast<size_t>(rank) * 2 + wg) * 32 * 128 + wg_thread;
+                constexpr size_t unit_float4 = kUnitPartialBytes / 16;
+                float4* mine_at = P.partials + static_cast<size_t>(u) * unit_float4 + wg * 32 * 128 + wg_thread;
 #pragma unroll
                 for (int i = 0; i < 32; ++i) {
                     __stcg(mine_at + i * 128, make_float4(acc[4 * i], acc[4 * i + 1], acc[4 * i + 2], acc[4 * i + 3]));
@@ -525,7 +498,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
                 __syncwarp();
                 int arrived = 0;
                 if (lane == 0) {
-                    int32_t* ticket = P.tickets + (static_cast<int64_t>(u / un.splits) * 2 + rank) * 8 + (warp - 4);
+                    int32_t* ticket = P.tickets + static_cast<int64_t>(u / un.splits) * 8 + (warp - 4);
                     arrived = atomicAdd(ticket, 1);
                     if (arrived == un.splits - 1) *ticket = 0;
                     __threadfence();
@@ -618,10 +591,9 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
     }
     tc_fence_before_sync();
     __syncthreads();
-    if (kPair) cluster_sync_all();
     if (warp == 1) {
         tc_fence_after_sync();
-        if (kPair) tmem_dealloc_pair(tmem_base, 512); else tmem_dealloc(tmem_base, 512);
+        tmem_dealloc(tmem_base, 512);
     }
 }
 
@@ -672,11 +644,8 @@ bool make_map(CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, ui
 }
 
 cudaError_t matmul_kernel_attributes() {
-    cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void*>(matmul_fp8_kernel<false>),
-                                         cudaFuncAttributeMaxDynamicSharedMemorySize, Geometry<false>::kSmem);
-    if (e != cudaSuccess) return e;
-    return cudaFuncSetAttribute(reinterpret_cast<const void*>(matmul_fp8_kernel<true>),
-                                cudaFuncAttributeMaxDynamicSharedMemorySize, Geometry<true>::kSmem);
+    return cudaFuncSetAttribute(reinterpret_cast<const void*>(matmul_fp8_kernel), cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                kSmemBytes);
 }
 
 int check_matmul(const monde_matmul_problem* p) {
@@ -699,7 +668,7 @@ bool aligned(const void* p, unsigned m) { return (reinterpret_cast<uintptr_t>(p)
 // Header as in the layer's workspace, then the parts of K-split tiles.
 size_t matmul_ws_bytes(const monde_matmul_problem&) { return WsLayout::kHidden + kMaxSplitUnits * kUnitPartialBytes; }
 static_assert(WsLayout::kHidden + kMaxSplitUnits * kUnitPartialBytes <= MONDE_MATMUL_WS_MAX, "workspace bound");
-static_assert(kMaxSplitUnits * 16 * 4 <= WsLayout::kPartDoneBytes, "tickets fit the header");
+static_assert(kMaxSplitUnits * 8 * 4 <= WsLayout::kPartDoneBytes, "tickets fit the header");
 
 int matmul(const monde_matmul_problem* p, const void* x, const float* x_scale, const void* w, const float* w_scale,
            const float* bias, bool grouped, const int32_t* offsets, const int32_t* row_ids, void* out, float* out_scale,
@@ -720,8 +689,6 @@ int matmul(const monde_matmul_problem* p, const void* x, const float* x_scale, c
     if (ws_bytes < matmul_ws_bytes(*p)) return MONDE_ERR_WORKSPACE;
     if ((st = check_arch()) != MONDE_OK) return st;
     if (per_device_once(kSetupMatmulFp8, matmul_kernel_attributes) != cudaSuccess) return MONDE_ERR_CUDA;
-    const DiagState diag = diag_state();
-    const bool pair = diag.ffn_pair > 0;
     const int64_t row_tiles = p->rows / 128 + static_cast<int64_t>(p->E) + 1, col_tiles = (p->N + kTileN - 1) / kTileN;
     if (row_tiles * col_tiles > (1 << 28) || static_cast<int64_t>(p->E) * p->N > 0x7fffff00 || p->K > 0x7fffff00 - 256)
         return MONDE_ERR_UNSUPPORTED;
@@ -742,7 +709,7 @@ int matmul(const monde_matmul_problem* p, const void* x, const float* x_scale, c
     P.status = reinterpret_cast<int32_t*>(base + WsLayout::kStatus);
     P.tickets = reinterpret_cast<int32_t*>(base + WsLayout::kPartDone);
     P.partials = reinterpret_cast<float4*>(base + WsLayout::kHidden);
-    P.wait_ns = diag.wait_limit_ns;
+    P.wait_ns = diag_state().wait_limit_ns;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     // A few rows: the kernel without tensor memory starts sooner and streams slower.  It is taken up to 32 MB of weights, where
     // eight rows more cost it as much as the weights again, and an e4m3 output as well.  (us, other kernel second: one row
@@ -777,13 +744,10 @@ int matmul(const monde_matmul_problem* p, const void* x, const float* x_scale, c
     MatmulMaps M;
     for (int i = 0; i < 3; ++i) {
         if (!make_map(&M.a[i], rows_at, rows_n, p->K, rows_ld, P.tma_gather ? 1 : kRowsPerCta >> i)) return MONDE_ERR_CUDA;
-        if (i < 2 && !make_map(&M.w[i], w, static_cast<uint64_t>(p->E) * p->N, p->K, p->K, (pair ? 128 : 256) >> i))
+        if (i < 2 && !make_map(&M.w[i], w, static_cast<uint64_t>(p->E) * p->N, p->K, p->K, kTileN >> i))
             return MONDE_ERR_CUDA;
     }
-    const int sms = current_sm_count();
-    const cudaError_t err = pair
-        ? launch_pdl_cluster(matmul_fp8_kernel<true>, dim3(sms & ~1), dim3(kThreads), Geometry<true>::kSmem, 2, s, M, P)
-        : launch_pdl(matmul_fp8_kernel<false>, dim3(sms), dim3(kThreads), Geometry<false>::kSmem, s, M, P);
+    const cudaError_t err = launch_pdl(matmul_fp8_kernel, dim3(current_sm_count()), dim3(kThreads), kSmemBytes, s, M, P);
     if (err != cudaSuccess) return MONDE_ERR_CUDA;
     return launched();
 }

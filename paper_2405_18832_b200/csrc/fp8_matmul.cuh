@@ -21,8 +21,8 @@ struct MatmulParams {
     int out_vec;                // rows of `out` start on 32-byte boundaries
     int bias_vec;               // rows of `bias` start on 16-byte boundaries
     int32_t* status;            // {status, site}
-    int32_t* tickets;           // [tile][CTA of the pair][epilogue warp]: parts of a K-split tile that have finished (zero between calls)
-    float4* partials;           // [unit][CTA of the pair][column half][32][128 threads]
+    int32_t* tickets;           // [tile][epilogue warp]: parts of a K-split tile that have finished (zero between calls)
+    float4* partials;           // [unit][column half][32][128 threads]
     unsigned long long wait_ns;
 };
 

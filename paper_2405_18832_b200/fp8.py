@@ -1,0 +1,154 @@
+"""The MoE FFN layer with 8-bit floating-point experts, put together from the calls of ``include/monde_fp8.h``.
+
+    residual += x;  h = rmsnorm(residual) * gamma                       monde_rmsnorm_quant (h in bf16 and in e4m3)
+    route h (bf16), find the expert order                               monde_route, monde_permute (ids alone)
+    u = act(h[rows of expert] W1^T + b1), re-quantised                  monde_grouped_matmul_fp8 (rows gathered by id)
+    y = u W2^T + b2                                                     monde_grouped_matmul_fp8
+    out[t] = sum_j w[t,j] y[rows of t]                                  monde_combine
+
+Expert weights are quantised once (``ExpertWeights``): half the bytes of the bf16 layer, which is what cold experts and
+decode batches are bound by.  ``python -m paper_2405_18832_b200.fp8 C1 C2 C3`` runs the named workloads in both forms and
+prints their device times and how far the outputs are apart.
+"""
+from __future__ import annotations
+
+import sys
+from typing import Optional
+
+import torch
+
+from . import binding as B
+from . import synthetic as S
+
+E4M3 = torch.float8_e4m3fn
+
+
+def _blocks(n: int) -> int:
+    return -(-n // B.FP8_BLOCK)
+
+
+def quantize_weights(w: torch.Tensor, stream=None):
+    """[..., N, K] float32 or bfloat16 -> (e4m3 values, scales per 128 x 128 block)."""
+    w = w.contiguous()
+    q = torch.empty(w.shape, dtype=E4M3, device=w.device)
+    scale = torch.empty((*w.shape[:-2], _blocks(w.shape[-2]), _blocks(w.shape[-1])), device=w.device)
+    B.monde_quantize_fp8(w, q, scale, B.FP8_BLOCK, stream)
+    return q, scale
+
+
+class ExpertWeights:
+    """W1 [E, d_ff, d_model] and W2 [E, d_model, d_ff] in e4m3, biases (or None) in float32."""
+
+    def __init__(self, W1, b1, W2, b2):
+        self.w1, self.w1_scale = quantize_weights(W1)
+        self.w2, self.w2_scale = quantize_weights(W2)
+        self.b1 = None if b1 is None else b1.float().contiguous()
+        self.b2 = None if b2 is None else b2.float().contiguous()
+
+
+class LayerBuffers(B.LayerBuffers):
+    """Device buffers of one layer call in this form (`p`: a bf16 problem), allocated once and reused."""
+
+    def __init__(self, p, device="cuda"):
+        super().__init__(p, device=device)
+        T, d, f, A = p.T, p.d_model, p.d_ff, p.T * p.top_k
+        self.x_perm = None                                   # rows are gathered where they lie
+        self.residual = torch.empty((T, d), dtype=torch.bfloat16, device=device)
+        self.h = torch.empty((T, d), dtype=torch.bfloat16, device=device)
+        self.q = torch.empty((T, d), dtype=E4M3, device=device)
+        self.q_scale = torch.empty((T, _blocks(d)), device=device)
+        self.u = torch.empty((A, f), dtype=E4M3, device=device)
+        self.u_scale = torch.empty((A, _blocks(f)), device=device)
+        size = max(B.monde_matmul_workspace_bytes(A, f, d, p.E, E4M3), B.monde_matmul_workspace_bytes(A, d, f, p.E))
+        if self.ws.numel() < size:                           # one workspace serves the layer's calls and the products
+            self.ws = torch.zeros(size, dtype=torch.uint8, device=device)
+
+
+def moe_ffn_layer_forward(p, x, residual: Optional[torch.Tensor], gamma, eps, Wg, bg, experts: ExpertWeights,
+                          buf: LayerBuffers, stream=None):
+    """Enqueues the layer on one stream; returns (out, residual): the layer's output and the updated residual stream, both
+    [T, d_model] bfloat16 in `buf`.  `residual` None: x alone starts the residual stream."""
+    B.monde_rmsnorm_quant(x, residual, gamma, eps, buf.residual, buf.h, buf.q, buf.q_scale, stream)
+    B.monde_route(p, buf.h, Wg, bg, buf.topk_idx, buf.topk_w, buf.counts, buf.offsets, buf.cls, buf.hot_ids, buf.cold_ids,
+                  buf.n_hot_cold, buf.probs, buf.ws, stream)
+    B.monde_permute(p, None, buf.topk_idx, buf.offsets, buf.perm, buf.inv_perm, None, buf.ws, stream)
+    B.monde_grouped_matmul_fp8(buf.q, buf.q_scale, experts.w1, experts.w1_scale, experts.b1, buf.offsets, buf.perm, buf.u,
+                               buf.u_scale, buf.ws, act=p.act, row_div=p.top_k, stream=stream)
+    B.monde_grouped_matmul_fp8(buf.u, buf.u_scale, experts.w2, experts.w2_scale, experts.b2, buf.offsets, None, buf.y_perm,
+                               None, buf.ws, stream=stream)
+    B.monde_combine(p, buf.y_perm, buf.inv_perm, buf.topk_w, buf.out, stream)
+    return buf.out, buf.residual
+
+
+class DenseFfn:
+    """A dense FFN in the same form (models of this kind alternate MoE and dense layers): weights quantised once, buffers
+    for up to `max_rows` rows."""
+
+    def __init__(self, W1, b1, W2, b2, max_rows: int, act: str = "relu"):
+        self.weights = ExpertWeights(W1, b1, W2, b2)
+        self.act = act
+        f, d = W1.shape
+        dev = W1.device
+        self.q = torch.empty((max_rows, d), dtype=E4M3, device=dev)
+        self.q_scale = torch.empty((max_rows, _blocks(d)), device=dev)
+        self.u = torch.empty((max_rows, f), dtype=E4M3, device=dev)
+        self.u_scale = torch.empty((max_rows, _blocks(f)), device=dev)
+        self.ws = torch.zeros(max(B.monde_matmul_workspace_bytes(max_rows, f, d), B.monde_matmul_workspace_bytes(max_rows, d, f)),
+                              dtype=torch.uint8, device=dev)
+
+    def forward(self, x, residual, gamma, eps, residual_out, out, stream=None) -> torch.Tensor:
+        """residual_out = x + residual; out = W2 act(W1 rmsnorm(residual_out) + b1) + b2, bfloat16."""
+        T, w = x.shape[0], self.weights
+        q, qs, u, us = self.q[:T], self.q_scale[:T], self.u[:T], self.u_scale[:T]
+        B.monde_rmsnorm_quant(x, residual, gamma, eps, residual_out, None, q, qs, stream)
+        B.monde_matmul_fp8(q, qs, w.w1, w.w1_scale, w.b1, u, us, self.ws, act=self.act, stream=stream)
+        B.monde_matmul_fp8(u, us, w.w2, w.w2_scale, w.b2, out, None, self.ws, stream=stream)
+        return out
+
+
+def _time_us(fn, repeats: int = 20) -> float:
+    flush = torch.empty(256 << 20, dtype=torch.uint8, device="cuda")       # larger than L2
+    times = []
+    for i in range(repeats + 3):
+        flush.zero_()
+        a, b = torch.cuda.Event(enable_timing=True), torch.cuda.Event(enable_timing=True)
+        a.record()
+        fn()
+        b.record()
+        torch.cuda.synchronize()
+        if i >= 3:
+            times.append(a.elapsed_time(b) * 1e3)
+    return sorted(times)[len(times) // 2]
+
+
+def compare(name: str) -> dict:
+    """One workload in both forms: device times with L2 flushed, and the relative distance of the outputs."""
+    w = S.config(name)
+    p = w.problem
+    g = {k: (None if v is None else v.cuda()) for k, v in S.generate(w, weights_device="cuda").items()}
+    gamma = torch.ones(p.d_model, dtype=torch.bfloat16, device="cuda")
+    experts = ExpertWeights(g["W1"], g["b1"], g["W2"], g["b2"])
+    buf8, buf16 = LayerBuffers(p), B.LayerBuffers(p)
+
+    def fp8():
+        moe_ffn_layer_forward(p, g["x"], None, gamma, 1e-6, g["Wg"], g["bg"], experts, buf8)
+
+    def bf16():                                              # the bf16 layer on the same normed rows
+        B.moe_ffn_layer_forward(p, buf8.h, g["Wg"], g["bg"], g["W1"], g["b1"], g["W2"], g["b2"], buf16,
+                                fuse_combine=B.fused_combine_wins(p))
+
+    fp8()
+    bf16()
+    torch.cuda.synchronize()
+    B.monde_poll_device_status(buf8.ws)
+    B.monde_poll_device_status(buf16.ws)
+    a, b = buf8.out.double(), buf16.out.double()
+    return {"workload": name, "fp8_us": _time_us(fp8), "bf16_us": _time_us(bf16),
+            "distance": float((a - b).norm() / b.norm())}
+
+
+if __name__ == "__main__":
+    for name in sys.argv[1:] or ["C1", "C2"]:
+        r = compare(name)
+        print("%-8s layer with e4m3 experts (norm included) %8.1f us, bf16 layer %8.1f us, outputs %.2f %% apart"
+              % (r["workload"], r["fp8_us"], r["bf16_us"], 100 * r["distance"]))

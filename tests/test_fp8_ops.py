@@ -265,7 +265,7 @@ def header_is_clean(ws):
 SIZES = [(1, 1, 16), (1, 128, 128), (1, 4096, 1024), (2, 129, 144), (15, 8, 32), (16, 256, 256), (17, 255, 112),
          (31, 1000, 2032), (33, 257, 272), (64, 640, 4096), (65, 127, 128), (100, 384, 512), (127, 128, 1024),
          (128, 256, 128), (129, 264, 384), (200, 136, 160), (257, 520, 256), (300, 1024, 768), (1000, 72, 2048),
-         (7, 2048, 8192), (513, 769, 1040)]
+         (7, 2048, 8192), (513, 769, 1040), (1300, 4096, 400), (3, 8192, 4096), (20, 1032, 528)]
 
 
 @pytest.mark.parametrize("rows,N,K", SIZES)
@@ -300,7 +300,8 @@ def split_rows(counts):
 
 GROUPS = [([0, 3, 0, 0, 129, 1, 64, 0], 256, 256, 2), ([1] * 5, 4096, 1024, 1), ([0, 0, 0, 700], 264, 400, 1),
           ([128, 128, 256], 512, 128, 1), ([17, 0, 33, 300, 2, 90], 1000, 1040, 2), ([0] * 60 + [1] + [0] * 194 + [5], 128, 64, 1),
-          ([2, 1, 3], 300, 8192, 4), ([0, 0], 128, 128, 1), ([500, 1, 1, 1, 260], 384, 640, 1)]
+          ([2, 1, 3], 300, 8192, 4), ([0, 0], 128, 128, 1), ([500, 1, 1, 1, 260], 384, 640, 1),
+          ([0, 1290, 30], 4096, 272, 2), ([3, 0, 2, 9, 0, 1, 7, 10], 520, 1040, 2), ([2000], 2048, 256, 1)]
 
 
 @pytest.mark.parametrize("counts,N,K,k", GROUPS)
