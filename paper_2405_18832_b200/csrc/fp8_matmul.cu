@@ -9,9 +9,10 @@
 // and the 1 x 128 block of an e4m3 output is one thread's registers.
 //
 // A work unit is (expert, row tile, 256 columns, K range).  Tiles of one expert follow one another, rows fastest in groups,
-// so the tiles that run at the same time share weights and rows through L2.  When there are too few tiles for the SMs the
-// K range is split: every part leaves its fp32 sums in the workspace and the part that finishes last (a counter per tile)
-// adds them in the order of K, whoever it is, so results are bit-reproducible and nobody waits.
+// so the tiles that run at the same time share weights and rows through L2.  The tiles left over from the last full round (all
+// of them, when there are few) may have their K range split: every part leaves its fp32 sums in the workspace and the part
+// that finishes last (a counter per tile) adds them in the order of K, whoever it is, so results are bit-reproducible and
+// nobody waits.
 #include <cuda.h>
 
 #include <algorithm>
@@ -62,14 +63,14 @@ __device__ __forceinline__ void give_up(int32_t* status, volatile int* abort_fla
 struct Tile {
     int e, r0, rows;      // expert, first row, rows of the tile
     int n0, cols;         // first column, columns
-    int tile, split;      // tile number, part of its K range
-    int kb0, kb1;
+    int kb0, kb1;         // K blocks
+    int parts, slot;      // parts of the tile's K range (1: all of it); place among the units that are parts
 };
 
 // The list of work units, the same in every CTA.  It stays in shared memory: a few registers more in every role made all of
 // them spill.
 struct Units {
-    int total, splits;              // units; parts per tile
+    int total, whole, splits;       // units; those that are whole tiles; parts of each further tile
     int tile_n, n_tiles, kb_all;    // columns of a tile, tiles of a row tile; K blocks
     uint32_t inverse[kMaxSplit + 1];    // ceil(2^32 / d)
     int prefix[kMaxExperts + 1];    // row tiles of the experts before e
@@ -77,17 +78,24 @@ struct Units {
     // Whole warps call.  (Divisions by numbers up to 16 are products with ceil(2^32 / d), exact below 2^28.)
     __device__ __forceinline__ Tile decode(int u, int lane, int E, int N, int tile_m) const {
         Tile t;
-        const int parts = splits;
-        t.tile = parts == 1 ? u : static_cast<int>(__umulhi(u, small_inverse(parts)));
-        t.split = u - t.tile * parts;
+        int tile = u, split = 0;
+        t.parts = 1;
+        t.slot = 0;
+        if (u >= whole) {
+            t.parts = splits;
+            t.slot = u - whole;
+            tile = t.parts == 1 ? t.slot : static_cast<int>(__umulhi(t.slot, small_inverse(t.parts)));
+            split = t.slot - tile * t.parts;
+            tile += whole;
+        }
         // the expert: the last one with prefix[e] * n_tiles <= tile (experts without rows have no tiles), by two ballots
         const int tiles = n_tiles;
-        const int coarse = __popc(__ballot_sync(0xffffffffu, lane * 8 < E && prefix[min(lane * 8, E)] * tiles <= t.tile)) - 1;
+        const int coarse = __popc(__ballot_sync(0xffffffffu, lane * 8 < E && prefix[min(lane * 8, E)] * tiles <= tile)) - 1;
         const int at = coarse * 8 + (lane & 7);
-        const unsigned fine = __ballot_sync(0xffffffffu, at < E && prefix[min(at, E)] * tiles <= t.tile);
+        const unsigned fine = __ballot_sync(0xffffffffu, at < E && prefix[min(at, E)] * tiles <= tile);
         t.e = coarse * 8 + __popc(fine & 0xffu) - 1;
         const int first_tile = prefix[t.e], m_tiles = prefix[t.e + 1] - first_tile;
-        int local = t.tile - first_tile * tiles, g = 0;
+        int local = tile - first_tile * tiles, g = 0;
         if (m_tiles > kRowGroup) {
             g = local / (kRowGroup * tiles);
             local -= g * kRowGroup * tiles;
@@ -101,9 +109,9 @@ struct Units {
         t.cols = min(tile_n, N - t.n0);
         t.kb0 = 0;
         t.kb1 = kb_all;
-        if (parts > 1) {                     // (K < 2^31, at most 16 parts: no overflow)
-            t.kb0 = static_cast<int>(__umulhi(kb_all * t.split, small_inverse(parts)));
-            t.kb1 = static_cast<int>(__umulhi(kb_all * (t.split + 1), small_inverse(parts)));
+        if (t.parts > 1) {                     // (K < 2^31, at most 16 parts: no overflow)
+            t.kb0 = static_cast<int>(__umulhi(kb_all * split, small_inverse(t.parts)));
+            t.kb1 = static_cast<int>(__umulhi(kb_all * (split + 1), small_inverse(t.parts)));
         }
         return t;
     }
@@ -243,13 +251,16 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
         const int row_tiles = prefix[P.E], wide = (P.N + kTileN - 1) / kTileN;
         const int tile_n = static_cast<int64_t>(row_tiles) * wide * 2 <= workers ? kTileN / 2 : kTileN;
         const int n_tiles = (P.N + tile_n - 1) / tile_n, kb_all = (P.K + kFp8Block - 1) / kFp8Block;
-        const int splits = P.may_split ? choose_splits(row_tiles * n_tiles, workers, kb_all, lane) : 1;
+        // rounds in which every CTA has a tile, and the tiles left over, which are split if that ends them sooner
+        const int tiles = row_tiles * n_tiles, whole = tiles / workers * workers;
+        const int splits = P.may_split && tiles > whole ? choose_splits(tiles - whole, workers, kb_all, lane) : 1;
         if (lane == 0) {
             un.tile_n = tile_n;
             un.n_tiles = n_tiles;
             un.kb_all = kb_all;
             un.splits = splits;
-            un.total = row_tiles * n_tiles * splits;
+            un.whole = whole;
+            un.total = whole + (tiles - whole) * splits;
         }
     }
     tc_fence_before_sync();
@@ -272,14 +283,10 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
 
     // K blocks of all of this CTA's units.
     const auto count_blocks = [&]() {
-        uint32_t n = 0;
-        if (un.splits == 1) {
-            if (worker < un.total) n = static_cast<uint32_t>((un.total - 1 - worker) / workers + 1) * un.kb_all;
-        } else {
-            for (int u = worker; u < un.total; u += workers) {
-                const Tile t = un.decode(u, lane, P.E, P.N, kRowsPerCta);
-                n += t.kb1 - t.kb0;
-            }
+        uint32_t n = static_cast<uint32_t>(un.whole / workers) * un.kb_all;       // (whole: a multiple of workers)
+        for (int u = un.whole + worker; u < un.total; u += workers) {
+            const Tile t = un.decode(u, lane, P.E, P.N, kRowsPerCta);
+            n += t.kb1 - t.kb0;
         }
         return n;
     };
@@ -386,7 +393,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
         float* const scale_buf = reinterpret_cast<float*>(staging + 8 * kStageWarpBytes + (warp - 4) * kScaleWarpBytes);
         const uint32_t tmem_mine = tmem_base + (static_cast<uint32_t>(quarter * 32) << 16) + wg * (kTileN / 2);
         const int nb = (P.N + kFp8Block - 1) / kFp8Block;
-        struct Part { int row0, warp_rows, n0, cols, e, kb0, kb1; };
+        struct Part { int row0, warp_rows, n0, cols, e, kb0, kb1, parts, slot; };
         const auto part_of = [&](const Tile& t) {
             Part p;
             p.row0 = t.r0 + quarter * 32;            // of the warp
@@ -396,6 +403,8 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
             p.e = t.e;
             p.kb0 = t.kb0;
             p.kb1 = t.kb1;
+            p.parts = t.parts;
+            p.slot = t.slot;
             return p;
         };
         // The scales of eight K blocks lie in a buffer of the warp, [32 rows + the weights'][8, padded to 9], those of the next
@@ -484,12 +493,12 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
                 }
             }
             // (after a wait that gave up what follows stores numbers that mean nothing, to the places they belong to)
-            if (un.splits > 1) {
+            if (t.parts > 1) {
                 // leave the sums; the part that comes last collects all of them in the order of K.  Every warp keeps its own
                 // counter: nothing here waits for another warp.
                 if (!active) continue;
                 constexpr size_t unit_float4 = kUnitPartialBytes / 16;
-                float4* mine_at = P.partials + static_cast<size_t>(u) * unit_float4 + wg * 32 * 128 + wg_thread;
+                float4* mine_at = P.partials + static_cast<size_t>(t.slot) * unit_float4 + wg * 32 * 128 + wg_thread;
 #pragma unroll
                 for (int i = 0; i < 32; ++i) {
                     __stcg(mine_at + i * 128, make_float4(acc[4 * i], acc[4 * i + 1], acc[4 * i + 2], acc[4 * i + 3]));
@@ -498,16 +507,16 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
                 __syncwarp();
                 int arrived = 0;
                 if (lane == 0) {
-                    int32_t* ticket = P.tickets + static_cast<int64_t>(u / un.splits) * 8 + (warp - 4);
+                    int32_t* ticket = P.tickets + static_cast<int64_t>(t.slot / t.parts) * 8 + (warp - 4);
                     arrived = atomicAdd(ticket, 1);
-                    if (arrived == un.splits - 1) *ticket = 0;
+                    if (arrived == t.parts - 1) *ticket = 0;
                     __threadfence();
                 }
-                if (__shfl_sync(0xffffffffu, arrived, 0) != un.splits - 1) continue;
+                if (__shfl_sync(0xffffffffu, arrived, 0) != t.parts - 1) continue;
 #pragma unroll
                 for (int i = 0; i < 128; ++i) acc[i] = 0.0f;
-                const float4* part = mine_at - static_cast<size_t>(u % un.splits) * unit_float4;
-                for (int s = 0; s < un.splits; ++s) {
+                const float4* part = mine_at - static_cast<size_t>(t.slot % t.parts) * unit_float4;
+                for (int s = 0; s < t.parts; ++s) {
 #pragma unroll
                     for (int i = 0; i < 32; ++i) {
                         const float4 v = __ldcg(part + i * 128);
@@ -720,24 +729,26 @@ int matmul(const monde_matmul_problem* p, const void* x, const float* x_scale, c
     if (p->rows <= kMatvecRows && matrices * p->N * p->K * passes <= (32 << 20)) return launch_matvec_fp8(P, w, s);
     // Rows picked by id: TMA's gather brings four rows in some 90 cycles, whatever their length, which passes unnoticed behind
     // the weights of a small tile but not at 128 rows (1.5 us per K block, twice the multiplication).  From 32 rows per expert
-    // on the rows are first copied side by side into the part of the workspace that K-split tiles would use, where there
-    // are too many tiles for a split and the copy fits.  128 experts 1024 -> 4096, gathered and copied: 16 rows each 96 and
+    // on the rows are first copied side by side into the workspace, behind the space for parts of tiles or, where the workspace
+    // ends before, in its place (tiles are not split then), if there are more tiles than SMs and the copy fits.  128 experts 1024 -> 4096, gathered and copied: 16 rows each 96 and
     // 100 us, 32 rows 99 and 102, 64 rows 126 and 116, 128 rows 185 and 134; 32 rows on average with a skewed router
     // (2048 -> 8192) 450 and 404.
     const size_t copy_bytes = static_cast<size_t>(p->rows) * p->K;
     const bool copy_rows = row_ids != nullptr && p->rows >= kCopyRowsPerExpert * p->E &&
                            p->rows / 128 * col_tiles > kMaxSplitUnits / 2 && copy_bytes <= ws_bytes - WsLayout::kHidden;
+    constexpr size_t kBehindParts = WsLayout::kHidden + kMaxSplitUnits * kUnitPartialBytes;
+    const bool behind = kBehindParts + copy_bytes <= ws_bytes;
+    uint8_t* const copy_at = reinterpret_cast<uint8_t*>(base) + (behind ? kBehindParts : WsLayout::kHidden);
     P.tma_gather = row_ids != nullptr && !copy_rows;
-    P.may_split = !copy_rows;
+    P.may_split = !copy_rows || behind;
     const void* rows_at = x;
     uint64_t rows_n = p->src_rows, rows_ld = p->ld_x;
     if (copy_rows) {
-        rows_at = base + WsLayout::kHidden;
+        rows_at = copy_at;
         rows_n = p->rows;
         rows_ld = p->K;
         const int64_t threads = static_cast<int64_t>(p->rows) * (p->K / 16);
-        if (launch_pdl(gather_rows_kernel, dim3(static_cast<unsigned>((threads + 255) / 256)), dim3(256), 0, s, P,
-                       reinterpret_cast<uint8_t*>(base) + WsLayout::kHidden) != cudaSuccess)
+        if (launch_pdl(gather_rows_kernel, dim3(static_cast<unsigned>((threads + 255) / 256)), dim3(256), 0, s, P, copy_at) != cudaSuccess)
             return MONDE_ERR_CUDA;
         count_launches(1);
     }
