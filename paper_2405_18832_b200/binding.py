@@ -234,14 +234,16 @@ _TORCH_DTYPE = {torch.float32: 0, torch.bfloat16: 1, torch.float8_e4m3fn: 2}
 _MATMUL_ACT = {"none": -1, "relu": 0, "gelu": 1}
 
 
-def _mat(name, t, rows, cols, dtype):
-    """Checks a [rows, cols] CUDA matrix with contiguous rows; returns its address and the distance between rows."""
-    if t.dtype is not dtype or t.shape != (rows, cols) or not t.is_cuda:
-        raise ValueError(f"{name}: expected a CUDA tensor [{rows}, {cols}] of {dtype}, got {t.device} {tuple(t.shape)} {t.dtype}")
+def _mat(name, t, shape, dtype):
+    """Checks a CUDA matrix of this shape with contiguous rows; returns its address and the distance between rows."""
+    if t.dtype is not dtype or t.shape != shape or not t.is_cuda:
+        raise ValueError(f"{name}: expected a CUDA tensor {tuple(shape)} of {dtype}, got {t.device} {tuple(t.shape)} {t.dtype}")
+    if t.is_contiguous():
+        return t.data_ptr(), shape[1]
     ld, one = t.stride()
-    if one != 1 and cols > 1:
+    if one != 1 and shape[1] > 1:
         raise ValueError(f"{name}: rows must be contiguous")
-    return t.data_ptr(), ld if rows > 1 else cols
+    return t.data_ptr(), ld if shape[0] > 1 else shape[1]
 
 
 def _dense(name, t, shape, dtype):
@@ -261,15 +263,15 @@ def _raw_stream(stream):
 def monde_rmsnorm_quant(x, residual, gamma, eps, residual_out, y, q, q_scale, stream=None) -> None:
     """v = x + residual; residual_out = v; u = v / sqrt(mean v^2 + eps) * gamma; y = u; q, q_scale = u as e4m3 with a
     scale per 1 x 128 block.  x [T, d] float32 or bfloat16; residual, gamma and each output may be None."""
-    T, d = x.shape
-    dt = x.dtype
-    px, lx = _mat("x", x, T, d, dt)
-    pr, lr = (0, 0) if residual is None else _mat("residual", residual, T, d, dt)
+    shape, dt = x.shape, x.dtype
+    T, d = shape
+    px, lx = _mat("x", x, shape, dt)
+    pr, lr = (0, 0) if residual is None else _mat("residual", residual, shape, dt)
     pg = 0 if gamma is None else _dense("gamma", gamma, (d,), dt)
-    po, lo = (0, 0) if residual_out is None else _mat("residual_out", residual_out, T, d, dt)
-    py, ly = (0, 0) if y is None else _mat("y", y, T, d, dt)
-    pq, lq = (0, 0) if q is None else _mat("q", q, T, d, torch.float8_e4m3fn)
-    ps, ls = (0, 0) if q_scale is None else _mat("q_scale", q_scale, T, -(-d // FP8_BLOCK), torch.float32)
+    po, lo = (0, 0) if residual_out is None else _mat("residual_out", residual_out, shape, dt)
+    py, ly = (0, 0) if y is None else _mat("y", y, shape, dt)
+    pq, lq = (0, 0) if q is None else _mat("q", q, shape, torch.float8_e4m3fn)
+    ps, ls = (0, 0) if q_scale is None else _mat("q_scale", q_scale, (T, -(-d // FP8_BLOCK)), torch.float32)
     st = lib().monde_rmsnorm_quant(_TORCH_DTYPE.get(dt, -1), T, d, eps, px, lx, pr, lr, pg, po, lo, py, ly, pq, lq, ps,
                                    ls, _raw_stream(stream))
     if st != 0:
@@ -289,9 +291,9 @@ def monde_quantize_fp8(x, q, q_scale, block_rows=1, stream=None) -> None:
         ls = -(-cols // FP8_BLOCK)
         ps = _dense("q_scale", q_scale, (batch, -(-rows // block_rows), ls), torch.float32)
     else:
-        px, lx = _mat("x", x, rows, cols, dt)
-        pq, lq = _mat("q", q, rows, cols, torch.float8_e4m3fn)
-        ps, ls = _mat("q_scale", q_scale, -(-rows // block_rows), -(-cols // FP8_BLOCK), torch.float32)
+        px, lx = _mat("x", x, x.shape, dt)
+        pq, lq = _mat("q", q, x.shape, torch.float8_e4m3fn)
+        ps, ls = _mat("q_scale", q_scale, (-(-rows // block_rows), -(-cols // FP8_BLOCK)), torch.float32)
     st = lib().monde_quantize_fp8(_TORCH_DTYPE.get(dt, -1), batch, rows, cols, block_rows, px, lx, pq, lq, ps, ls,
                                   _raw_stream(stream))
     if st != 0:
@@ -312,15 +314,15 @@ def _matmul(name, x, x_scale, w, w_scale, bias, offsets, row_ids, out, out_scale
     E = w.shape[0] if grouped else 1
     kb, nb = -(-K // FP8_BLOCK), -(-N // FP8_BLOCK)
     e4m3, f32 = torch.float8_e4m3fn, torch.float32
-    px, lx = _mat("x", x, src_rows, K, e4m3)
-    pxs, lxs = _mat("x_scale", x_scale, src_rows, kb, f32)
+    px, lx = _mat("x", x, (src_rows, K), e4m3)
+    pxs, lxs = _mat("x_scale", x_scale, (src_rows, kb), f32)
     lead = (E,) if grouped else ()
     pw = _dense("w", w, lead + (N, K), e4m3)
     pws = _dense("w_scale", w_scale, lead + (nb, kb), f32)
     pb = 0 if bias is None else _dense("bias", bias, lead + (N,), f32)
     dt = out.dtype
-    po, lo = _mat("out", out, rows, N, dt)
-    pos, los = (0, 0) if out_scale is None else _mat("out_scale", out_scale, rows, nb, f32)
+    po, lo = _mat("out", out, (rows, N), dt)
+    pos, los = (0, 0) if out_scale is None else _mat("out_scale", out_scale, (rows, nb), f32)
     cp = monde_matmul_problem(rows, N, K, E, src_rows, row_div, _MATMUL_ACT[act],
                               _TORCH_DTYPE.get(dt, -1), lx, lxs, lo, los)
     ref = ctypes.byref(cp)

@@ -45,10 +45,10 @@ __global__ void __launch_bounds__(kNormMaxThreads) rmsnorm_quant_kernel(const No
     Raw8<T> xr[CH], rr[CH], gr[CH];
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-        const int c = (i * blockDim.x + tid) * 8;
-        xr[i].template load<kVec>(x + c, P.d - c);
-        if (res != nullptr) rr[i].template load<kVec>(res + c, P.d - c);
-        if (gamma != nullptr) gr[i].template load<kVec>(gamma + c, P.d - c);
+        const int c = first_column<kVec, 16>(i * blockDim.x + tid);
+        xr[i].template load<kVec, 16>(x + c, P.d - c);
+        if (res != nullptr) rr[i].template load<kVec, 16>(res + c, P.d - c);
+        if (gamma != nullptr) gr[i].template load<kVec, 16>(gamma + c, P.d - c);
     }
     float v[CH][8];
     float sum = 0.0f;
@@ -63,8 +63,8 @@ __global__ void __launch_bounds__(kNormMaxThreads) rmsnorm_quant_kernel(const No
     if (P.residual_out != nullptr) {
 #pragma unroll
         for (int i = 0; i < CH; ++i) {
-            const int c = (i * blockDim.x + tid) * 8;
-            if (c < P.d) store8<T, kVec>(static_cast<T*>(P.residual_out) + row * P.ld_residual_out + c, P.d - c, v[i]);
+            const int c = first_column<kVec, 16>(i * blockDim.x + tid);
+            if (c < P.d) store8<T, kVec, 16>(static_cast<T*>(P.residual_out) + row * P.ld_residual_out + c, P.d - c, v[i]);
         }
     }
     // t = v * gamma.  u = t * rms differs from t by one factor for the whole row, and so does a block's amax: q = u / scale
@@ -72,7 +72,7 @@ __global__ void __launch_bounds__(kNormMaxThreads) rmsnorm_quant_kernel(const No
     float amax[CH];
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-        const int c = (i * blockDim.x + tid) * 8;
+        const int c = first_column<kVec, 16>(i * blockDim.x + tid);
         amax[i] = 0.0f;
         if (c >= P.d) continue;
 #pragma unroll
@@ -93,7 +93,7 @@ __global__ void __launch_bounds__(kNormMaxThreads) rmsnorm_quant_kernel(const No
     const float rms = __frsqrt_rn(__fdiv_rn(sum, static_cast<float>(P.d)) + P.eps);
 #pragma unroll
     for (int i = 0; i < CH; ++i) {
-        const int c = (i * blockDim.x + tid) * 8;
+        const int c = first_column<kVec, 16>(i * blockDim.x + tid);
         const bool in = c < P.d;
         if (P.q != nullptr) {
             const float a = half_warp_max(amax[i]);
@@ -102,14 +102,14 @@ __global__ void __launch_bounds__(kNormMaxThreads) rmsnorm_quant_kernel(const No
             // a block too small for a scale is zeros; a NaN in the row (rms is NaN) reaches every block
             const float f = ua >= kTinyAmax ? __fdiv_rn(kE4m3Max, a) : ua * 0.0f;
             if (in) {
-                store8_e4m3<kVec>(P.q + row * P.ld_q + c, P.d - c, v[i], f);
+                store8_e4m3<kVec, 16>(P.q + row * P.ld_q + c, P.d - c, v[i], f);
                 if ((lane & 15) == 0) P.scale[row * P.ld_scale + c / kFp8Block] = s;
             }
         }
         if (in && P.y != nullptr) {
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[i][j] *= rms;
-            store8<T, kVec>(static_cast<T*>(P.y) + row * P.ld_y + c, P.d - c, v[i]);
+            store8<T, kVec, 16>(static_cast<T*>(P.y) + row * P.ld_y + c, P.d - c, v[i]);
         }
     }
 }
@@ -144,10 +144,10 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const QuantParams P)
     for (int i = 0; i < kRowsInFlight; ++i) {
         const uint32_t b = b0 + i * groups;
         row[i] = b / static_cast<uint32_t>(P.blocks);
-        c[i] = b < total ? static_cast<int>(b - row[i] * P.blocks) * kFp8Block + lane * 8 : P.cols;
+        c[i] = b < total ? static_cast<int>(b - row[i] * P.blocks) * kFp8Block + (kVec ? lane * 8 : lane) : P.cols;
         const T* src = static_cast<const T*>(P.x) + row[i] * P.ld_x + c[i];
-        x[i][0].template load<kVec>(src, P.cols - c[i]);
-        x[i][1].template load<kVec>(src + 64, P.cols - c[i] - 64);
+        x[i][0].template load<kVec, 8>(src, P.cols - c[i]);
+        x[i][1].template load<kVec, 8>(src + 64, P.cols - c[i] - 64);
     }
 #pragma unroll
     for (int i = 0; i < kRowsInFlight; ++i) {
@@ -163,7 +163,7 @@ __global__ void __launch_bounds__(256) quantize_rows_kernel(const QuantParams P)
             float v[8];
 #pragma unroll
             for (int j = 0; j < 8; ++j) v[j] = x[i][h][j];
-            store8_e4m3<kVec>(q + h * 64, n, v, inv);
+            store8_e4m3<kVec, 8>(q + h * 64, n, v, inv);
         }
         if (lane == 0 && c[i] < P.cols) P.scale[row[i] * P.ld_scale + c[i] / kFp8Block] = s;
     }
@@ -184,13 +184,13 @@ __global__ void __launch_bounds__(256, 4) quantize_blocks_kernel(const QuantPara
     const int cb = static_cast<int>(tile - rb * P.blocks);
     const int64_t batch = rb / row_blocks;
     const int r0 = static_cast<int>(rb - batch * row_blocks) * kFp8Block;
-    const int c = cb * kFp8Block + (tid & 15) * 8;
+    const int c = cb * kFp8Block + first_column<kVec, 16>(tid & 15);
     const int64_t row0 = batch * P.rows_each + r0 + (tid >> 4);
     const int rows = c < P.cols ? P.rows_each - r0 - (tid >> 4) : 0;      // this thread's rows: i with 16 * i < rows
     const T* x = static_cast<const T*>(P.x) + row0 * P.ld_x + c;
     Raw8<T> raw[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) raw[i].template load<kVec>(x + i * 16 * P.ld_x, 16 * i < rows ? P.cols - c : 0);
+    for (int i = 0; i < 8; ++i) raw[i].template load<kVec, 16>(x + i * 16 * P.ld_x, 16 * i < rows ? P.cols - c : 0);
     float amax = raw[0].amax();
 #pragma unroll
     for (int i = 1; i < 8; ++i) amax = max_nan(amax, raw[i].amax());
@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(256, 4) quantize_blocks_kernel(const QuantPara
         float v[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] = raw[i][j];
-        store8_e4m3<kVec>(P.q + (row0 + i * 16) * P.ld_q + c, P.cols - c, v, inv);
+        store8_e4m3<kVec, 16>(P.q + (row0 + i * 16) * P.ld_q + c, P.cols - c, v, inv);
     }
     if (tid == 0) P.scale[rb * P.ld_scale + cb] = s;
 }
