@@ -921,10 +921,11 @@ int matmul(const monde_matmul_problem* p, const void* x, const float* x_scale, c
         if (i < 2 && !make_map(&M.w[i], w, static_cast<uint64_t>(p->E) * p->N, p->K, p->K, kTileN >> i))
             return MONDE_ERR_CUDA;
     }
-    // Turning cold tiles round costs the other tiles a few per cent (a larger kernel) and 32 rows more time at the end of a tile
-    // than it saves where K is short.  Layers of 64 experts 1024 -> 4096 -> 1024, us without and with: 2 rows per expert on
-    // average 95 and 87, 16 rows 170 and 162, 32 rows 172 and 172, 64 rows 203 and 212; decode step on 27 of 128 experts
-    // 1024 -> 4096 29.3 and 25.6; 32 rows on 128 experts 2048 -> 8192, skewed, 420 and 397.
+    // A kernel that can turn tiles round is slower on the tiles that it does not turn (16384 x 8192 x 2048: 387 us without,
+    // 408 with), and a turned tile of 32 rows with a short K has a longer end (37 experts, 4096 x 512, e4m3: 24 and 32).
+    // Layers of 64 experts 1024 -> 4096 -> 1024, us without and with: 2 rows per expert on average 95 and 87, 16 rows 170
+    // and 162, 32 rows 172 and 172, 64 rows 203 and 212.  Products: 32 rows spread over 128 experts, 1024 -> 4096, 29.3 and
+    // 25.6; 32 rows per expert on average, skewed over 128 experts, 2048 -> 8192, 420 and 397.
     const bool cold = p->rows <= static_cast<int64_t>(kColdRowsPerExpert) * p->E;
     const cudaError_t err = launch_pdl(cold ? matmul_fp8_kernel<true> : matmul_fp8_kernel<false>, dim3(current_sm_count()), dim3(kThreads), kSmemBytes, s, M, P);
     if (err != cudaSuccess) return MONDE_ERR_CUDA;
