@@ -217,7 +217,8 @@ def operands(seed, src_rows, N, K, E=None):
 def activate(z, act):
     if act == "relu":
         return z.clamp(min=0)
-    return 0.5 * z * (1 + torch.erf(z * math.sqrt(0.5))) if act == "gelu" else z
+    # erfc, as 1 + erf cancels to zero below -8.3 and a block whose values all lie there has a scale of its own
+    return 0.5 * z * torch.special.erfc(z * -math.sqrt(0.5)) if act == "gelu" else z
 
 
 def product_ref(x, xs, w, ws, b, act):
@@ -396,6 +397,84 @@ def test_non_finite_rows_blocks_and_experts_do_not_leak(out, act):
         assert c[3:133, 130].isnan().all()
     assert torch.equal(a[~touched], c[~touched])
     assert c[2].isnan().all() and c[60].isnan().all() and not torch.isfinite(c[140]).all()
+
+
+# Few rows per expert on average (at most 32): tiles of at most 32 rows take another path through the big kernel than the
+# rest.  Row counts on both sides of its tile size, ragged N and K, few tiles with a long K (their K range is split).
+TURNED = [([31, 32, 33, 0, 1, 64, 8, 9], 264, 528), ([32] * 8, 256, 128), ([0, 129, 1, 2, 0, 0, 16, 17], 130, 1040),
+          ([5, 0, 28, 1], 1032, 4112), ([160, 0, 0, 0, 0, 32], 392, 272), ([33, 0], 8, 16)]
+
+
+@pytest.mark.parametrize("counts,N,K", TURNED)
+@pytest.mark.parametrize("out", ["bf16", "f32", "e4m3"])
+@pytest.mark.parametrize("act", ["none", "relu", "gelu"])
+@pytest.mark.parametrize("gather", [False, True])
+def test_grouped_product_with_few_rows_per_expert(counts, N, K, out, act, gather):
+    E, A, k = len(counts), sum(counts), 2
+    assert 32 < A <= 32 * E
+    off = split_rows(counts)
+    src_rows = A // k + 1 if gather else A
+    x, xs, w, ws, b = operands(A + N + K, src_rows, N, K, E)
+    ids = torch.randint(0, src_rows * k, (A,), generator=gen(5), dtype=torch.int32)
+    src = ids.long() // k if gather else torch.arange(A)
+    wk = workspace(A, N, K, E)
+    for pad in (0, 3):
+        o, o_raw = padded(A, N, DT[out], pad)
+        os_, os_raw = padded(A, up(N), torch.float32, pad)
+        B.monde_grouped_matmul_fp8(x.cuda(), xs.cuda(), w.cuda(), ws.cuda(), b.cuda(), off.cuda(),
+                                   ids.cuda() if gather else None, o, os_ if out == "e4m3" else None, wk, act=act, row_div=k)
+        B.monde_poll_device_status(wk)
+        for e in range(E):
+            r = slice(int(off[e]), int(off[e + 1]))
+            if r.start < r.stop:
+                ref, tol = product_ref(x[src[r]], xs[src[r]], w[e], ws[e], b[e], act)
+                check_out(o[r], os_[r], ref, tol)
+        assert untouched(o, o_raw) and untouched(os_, os_raw) and header_is_clean(wk)
+
+
+@pytest.mark.parametrize("rows,N,K", [(9, 8200, 4112), (32, 4100, 4096), (32, 20000, 528)])
+@pytest.mark.parametrize("out", ["bf16", "f32", "e4m3"])
+def test_product_of_few_rows_with_many_weights(rows, N, K, out):
+    x, xs, w, ws, b = operands(rows + N, rows, N, K)
+    ref, tol = product_ref(x, xs, w, ws, b, "relu")
+    wk = workspace(rows, N, K)
+    o, s = torch.empty(rows, N, dtype=DT[out], device="cuda"), torch.empty(rows, up(N), device="cuda")
+    B.monde_matmul_fp8(x.cuda(), xs.cuda(), w.cuda(), ws.cuda(), b.cuda(), o, s if out == "e4m3" else None, wk, act="relu")
+    B.monde_poll_device_status(wk)
+    check_out(o, s, ref, tol)
+    assert header_is_clean(wk)
+
+
+@pytest.mark.parametrize("out", ["bf16", "e4m3"])
+@pytest.mark.parametrize("act", ["none", "relu", "gelu"])
+def test_non_finite_values_in_tiles_of_few_rows_do_not_leak(out, act):
+    counts, N, K = [3, 30, 0, 20], 384, 512
+    off, A = split_rows(counts), sum(counts)
+    x, xs, w, ws, b = operands(4, A, N, K, 4)
+    results = []
+    for poison in (False, True):
+        if poison:
+            x.view(torch.uint8)[2, 100] = 0x7f           # NaN in the last row of expert 0
+            xs[40, 1] = float("inf")                     # an infinite scale in expert 3's rows
+            xs[20, 3] = float("nan")
+            w.view(torch.uint8)[2] = 0x7f                # an expert without rows: all NaN
+            ws[2] = float("nan")
+            w.view(torch.uint8)[1, 130, 5] = 0xff        # one output column of expert 1
+        wk = workspace(A, N, K, 4)
+        o, s = torch.zeros(A, N, dtype=DT[out], device="cuda"), torch.zeros(A, 3, device="cuda")
+        B.monde_grouped_matmul_fp8(x.cuda(), xs.cuda(), w.cuda(), ws.cuda(), b.cuda(), off.cuda(), None, o,
+                                   s if out == "e4m3" else None, wk, act=act)
+        B.monde_poll_device_status(wk)
+        v = o.float().cpu()
+        results.append(v * expand(s.cpu(), A, N) if out == "e4m3" else v)
+    a, c = results
+    touched = torch.zeros(A, N, dtype=torch.bool)
+    touched[[2, 40, 20]] = True
+    columns = slice(128, 256) if out == "e4m3" else slice(130, 131)      # the block that shares the column's scale
+    touched[3:33, columns] = True
+    assert not torch.isfinite(c[3:33, columns]).any()
+    assert torch.equal(a[~touched], c[~touched])
+    assert c[2].isnan().all() and c[20].isnan().all() and not torch.isfinite(c[40]).all()
 
 
 def test_same_bits_every_time_and_on_another_stream():
