@@ -18,6 +18,12 @@ __device__ __forceinline__ float max_nan(float a, float b) {
     asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
+// The same with the magnitudes of two more values.
+__device__ __forceinline__ float max_nan_abs(float a, float b, float c) {
+    float r;
+    asm("max.NaN.abs.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+    return r;
+}
 // amax / 448, or 1 for a block too small to divide by (the reciprocal of any other scale is a normal number).
 // Both are kept in fp32: a scale rounded to fewer bits would add its error to all 128 values.
 __device__ __forceinline__ float block_scale(float amax) {
@@ -44,7 +50,7 @@ __device__ __forceinline__ float2 gelu2(float2 v) {
     float2 q;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(q.x) : "f"(r.x));
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(q.y) : "f"(r.y));
-    return make_float2(fmaf(-z.x, q.x, max_nan(v.x, 0.0f)), fmaf(-z.y, q.y, max_nan(v.y, 0.0f)));
+    return __ffma2_rn(make_float2(-z.x, -z.y), q, make_float2(max_nan(v.x, 0.0f), max_nan(v.y, 0.0f)));
 }
 // Four values to e4m3, round to nearest even; the largest of a block lands on 448 (one rounding step of the product above
 // it at most, which rounds back), so nothing saturates.

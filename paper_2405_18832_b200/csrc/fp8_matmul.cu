@@ -736,7 +736,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
                 float amax = 0.0f;
                 if (cols == kFp8Block) {
 #pragma unroll
-                    for (int i = 0; i < 128; ++i) amax = max_nan(amax, fabsf(v[i]));
+                    for (int i = 0; i < 128; i += 2) amax = max_nan_abs(amax, v[i], v[i + 1]);
                 } else {
 #pragma unroll
                     for (int i = 0; i < 128; ++i)
@@ -746,7 +746,9 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
                 if (lane < warp_rows) P.out_scale[(row0 + lane) * P.ld_out_scale + n0 / kFp8Block] = s;
                 store_rows<1>(stage_out, static_cast<uint8_t*>(P.out) + row0 * P.ld_out + n0, P.ld_out, warp_rows, cols,
                               P.out_vec, lane, [&](int i) {
-                                  return pack_e4m3(v[4 * i] * inv, v[4 * i + 1] * inv, v[4 * i + 2] * inv, v[4 * i + 3] * inv);
+                                  const float2 k2 = make_float2(inv, inv), lo = __fmul2_rn(make_float2(v[4 * i], v[4 * i + 1]), k2),
+                                               hi = __fmul2_rn(make_float2(v[4 * i + 2], v[4 * i + 3]), k2);
+                                  return pack_e4m3(lo.x, lo.y, hi.x, hi.y);
                               });
             }
         }
