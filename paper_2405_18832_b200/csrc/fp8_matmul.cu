@@ -52,9 +52,9 @@ constexpr size_t kUnitPartialBytes = size_t(kRowsPerCta) * kTileN * 4;
 constexpr int kStageWarpBytes = 32 * 16;                            // output rows that cannot go out straight
 constexpr int kColdRowsPerExpert = 32;     // with up to so many on average cold tiles are turned round
 constexpr int kColdRows = 32;          // tiles of at most so many rows are multiplied with the weights as the MMA's rows
-// Scales of eight K blocks, twice: [32 rows and the weights'][8, padded to 9], for a cold tile [8][32 rows, padded to 36] and
-// the weights'.
-constexpr int kScalePitch = 9, kColdPitch = 36, kScaleHalf = 300;
+// Scales of eight K blocks, twice: [32 rows and the weights'][8], the halves of four swapped where the row's bit 2 is set
+// (lanes read a column, which would meet in four banks), for a cold tile [8][32 rows, padded to 36] and the weights'.
+constexpr int kScalePitch = 8, kColdPitch = 36, kScaleHalf = 296;
 static_assert(kScaleHalf >= 33 * kScalePitch && kScaleHalf >= 8 * kColdPitch + 8 && kScaleHalf % 4 == 0, "scale buffers");
 constexpr int kScaleWarpBytes = 2 * kScaleHalf * 4;
 constexpr int kCopyRowsPerExpert = 32;   // from here on rows picked by id are copied first
@@ -431,22 +431,35 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
             p.slot = t.slot;
             return p;
         };
-        // The scales of eight K blocks lie in a buffer of the warp, [32 rows + the weights'][8, padded to 9], those of the next
-        // eight (of the next tile, at the end) are on their way to its other half.  Eight lanes read a row's scales: four
-        // lines per load, where a lane per row took 32, one after the other, with the barriers of the other warps behind.
+        // The scales of eight K blocks lie in a buffer of the warp, those of the next eight (of the next tile, at the end) are on
+        // their way to its other half.  Eight lanes read a row's scales one by one, or where rows are aligned two lanes four
+        // each: a copy instruction costs the SM's eight epilogue warps some 27 cycles each whatever its width, 1750 cycles for
+        // eight K blocks in one form and 740 in the other (8 experts x 2048 rows, 8192 -> 2048: 304 and 290 us).
         int half = 0;
         const auto load_scales = [&](const Part& p, int src, int kb, int to) {
             const int at = kb + (lane & 7);
             const bool active = p.warp_rows > 0 && p.cols > 0;
-            const int r_step = p.cold ? 1 : kScalePitch;
-            float* const dst = scale_buf + to * kScaleHalf + (lane & 7) * (p.cold ? kColdPitch : 1);
+            float* const to_buf = scale_buf + to * kScaleHalf;
+            if (P.scale_vec && !p.cold && (kb & 3) == 0) {
+                const int c = (lane & 1) * 4, left = min(p.kb1 - (kb + c), 4);
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int r = 4 * j + (lane >> 3), s = __shfl_sync(0xffffffffu, src, r);
-                if (s >= 0 && at < p.kb1) copy_async_4(dst + r * r_step, P.x_scale + s * P.ld_x_scale + at);
+                for (int j = 0; j < 2; ++j) {
+                    const int r = 16 * j + (lane >> 1), s = __shfl_sync(0xffffffffu, src, r);
+                    if (s >= 0 && left > 0)
+                        copy_async_16(to_buf + r * kScalePitch + (c ^ (r & 4)), P.x_scale + s * P.ld_x_scale + kb + c, left * 4);
+                }
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    const int r = 4 * j + (lane >> 3), i = lane & 7, s = __shfl_sync(0xffffffffu, src, r);
+                    if (s >= 0 && at < p.kb1)
+                        copy_async_4(to_buf + (p.cold ? i * kColdPitch + r : r * kScalePitch + (i ^ (r & 4))),
+                                     P.x_scale + s * P.ld_x_scale + at);
+                }
             }
             if (lane < 8 && active && at < p.kb1)
-                copy_async_4(p.cold ? scale_buf + to * kScaleHalf + 8 * kColdPitch + lane : dst + 32 * kScalePitch, P.w_scale + (static_cast<int64_t>(p.e) * nb + p.n0 / kFp8Block) * un.kb_all + at);
+                copy_async_4(to_buf + (p.cold ? 8 * kColdPitch : 32 * kScalePitch) + lane,
+                             P.w_scale + (static_cast<int64_t>(p.e) * nb + p.n0 / kFp8Block) * un.kb_all + at);
             copy_async_commit();
         };
         // A tile is found, and its row ids are asked for, one tile ahead.
@@ -620,7 +633,7 @@ __global__ void __launch_bounds__(kThreads, 1) matmul_fp8_kernel(const __grid_co
                     }
                     const int blocks = min(8, t.kb1 - c0);
                     for (int i = 0; i < blocks; ++i) {
-                        const float f = sc[lane * kScalePitch + i] * sc[32 * kScalePitch + i];
+                        const float f = sc[lane * kScalePitch + (i ^ (lane & 4))] * sc[32 * kScalePitch + i];
                         const int b = n++ & 1;
                         named_sync(kBarFull + 2 * b + wg, kFullThreads);
                         tc_fence_after_sync();
@@ -880,6 +893,7 @@ int matmul(const monde_matmul_problem* p, const void* x, const float* x_scale, c
     P.out_scale = out_scale;
     P.out_vec = aligned(out, 32) && (p->ld_out * ob) % 32 == 0;
     P.bias_vec = aligned(bias, 16) && p->N % 4 == 0;
+    P.scale_vec = aligned(x_scale, 16) && p->ld_x_scale % 4 == 0;
     P.status = reinterpret_cast<int32_t*>(base + WsLayout::kStatus);
     P.tickets = reinterpret_cast<int32_t*>(base + WsLayout::kPartDone);
     P.partials = reinterpret_cast<float4*>(base + WsLayout::kHidden);

@@ -20,6 +20,7 @@ struct MatmulParams {
     int tma_gather;             // rows of x are picked by id while they are loaded (else: they lie in order)
     int out_vec;                // rows of `out` start on 32-byte boundaries
     int bias_vec;               // rows of `bias` start on 16-byte boundaries
+    int scale_vec;              // rows of x_scale start on 16-byte boundaries
     int32_t* status;            // {status, site}
     int32_t* tickets;           // [tile][epilogue warp]: parts of a K-split tile that have finished (zero between calls)
     float4* partials;           // [unit][column half][32][128 threads]
