@@ -51,6 +51,7 @@ int monde_rmsnorm_quant(int32_t dtype, int32_t T, int32_t d, float eps, const vo
  * 128 (weights; a block never spans two matrices of the batch).
  * in : x [batch, rows, cols] (dtype MONDE_F32 or MONDE_BF16), rows ld_x elements apart, matrices rows * ld_x
  * out: q [batch, rows, cols] e4m3, rows ld_q apart; scale [batch, ceil(rows/block_rows), ceil(cols/128)], rows ld_scale apart
+ * Limits: fewer than 2^31 blocks in all, otherwise MONDE_ERR_UNSUPPORTED.
  */
 int monde_quantize_fp8(int32_t dtype, int32_t batch, int32_t rows, int32_t cols, int32_t block_rows, const void* x,
                        int64_t ld_x, void* q, int64_t ld_q, float* scale, int64_t ld_scale, void* stream);
@@ -94,7 +95,8 @@ int monde_matmul_fp8(const monde_matmul_problem* p, const void* x, const float* 
  * in : w [E,N,K], w_scale [E, ceil(N/128), ceil(K/128)], bias [E,N] or NULL; offsets [E+1] int32 ascending, as written by
  *      monde_route; row_ids [rows] int32 or NULL (position r reads row r of x) - monde_permute's perm, with
  *      row_div = top_k, reads every token's row where it lies, so no permuted copy is needed.
- * Limits: E <= 256.
+ * Limits, here and above: K a multiple of 16, E <= 256, E * N < 2^31 - 256, (rows/128 + E + 1) * ceil(N/256) <= 2^28;
+ * otherwise MONDE_ERR_UNSUPPORTED.
  */
 int monde_grouped_matmul_fp8(const monde_matmul_problem* p, const void* x, const float* x_scale, const void* w,
                              const float* w_scale, const float* bias, const int32_t* offsets, const int32_t* row_ids,

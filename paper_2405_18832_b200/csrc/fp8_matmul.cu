@@ -16,6 +16,14 @@
 // of them, when there are few) may have their K range split: every part leaves its fp32 sums in the workspace and the part
 // that finishes last (a counter per tile) adds them in the order of K, whoever it is, so results are bit-reproducible and
 // nobody waits.
+//
+// What bounds it.  Many rows: 8 experts x 2048 rows 8192 -> 2048 take 290-303 us (1.81-1.90 PFLOP/s).  A K block takes about 910
+// cycles where its MMAs need 512; the epilogue never waits for one, so its own work is the measure: 550 cycles to read and add a
+// block (tensor memory 240 and packed additions 280 by themselves), the rest barriers, scales and a tile's end.  In runs of
+// seconds the power limit holds the SM clock at 1.37 GHz (359 us).  16384 x 8192 x 2048 to e4m3 with GELU 363-370 us: a tile's
+// end is some 9000 cycles (GELU 3800, the row's scale and stores 2900, finding the next tile 1000), and behind it only two K
+// blocks are multiplied.  Few rows per expert: the weights from HBM, 2.2 GB in 382-390 us (5.6-5.8 TB/s; 128 experts, 2048
+// tokens top-2, skewed); 27 experts 1024 -> 4096 25.8 us (4.6 TB/s), some 5 us of them the way in and out of the kernel.
 #include <cuda.h>
 
 #include <algorithm>
@@ -909,19 +917,21 @@ int matmul(const monde_matmul_problem* p, const void* x, const float* x_scale, c
     P.partials = reinterpret_cast<float4*>(base + WsLayout::kHidden);
     P.wait_ns = diag_state().wait_limit_ns;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
-    // A few rows: the kernel without tensor memory starts sooner and streams slower.  It is taken up to 32 MB of weights, where
-    // eight rows more cost it as much as the weights again, and an e4m3 output as well.  (us, other kernel second: one row
-    // 4096 x 4096 8.6 and 21.1, 8192 x 8192 20.5 and 24.3; 4 of 128 experts 1024 -> 4096 9.2 and 11; 27 of them 38.6 and 27.9,
-    // with an e4m3 output 74.9 and 29.5.)
-    const int64_t matrices = grouped ? std::min(p->E, p->rows) : 1;
-    const int64_t passes = (grouped || p->rows <= 8 ? 1 : p->rows <= 16 ? 2 : 4) * (p->out_dtype == MONDE_E4M3 ? 2 : 1);
-    if (p->rows <= kMatvecRows && matrices * p->N * p->K * passes <= (32 << 20)) return launch_matvec_fp8(P, w, s);
+    // A few rows: the kernel without tensor memory starts sooner and streams slower.  It is taken up to 8 MB of weights, where
+    // its CTAs (clusters of eight for an e4m3 output) are all resident at once, and up to 16 MB for at most 16 rows that are not
+    // quantised.  us, this kernel and the other: one row 1024 -> 4096 4.8 and 7.7, 2048 -> 4096 5.4 and 10.6, 4096 -> 4096 8.8
+    // and 11.9 (e4m3 14.9 and 12.2), 5120 -> 5120 14.6 and 13.8; 16 rows 4096 -> 4096 10.7 and 12.8; 32 rows 2048 -> 4096 9.2
+    // and 12.2 (e4m3 11.2 and 13.9), 2048 -> 6144 16.0 and 12.8.  Experts 1024 -> 4096, one row each: two 5.8 and 8.0 (e4m3 6.7
+    // and 8.3), four 9.2 and 8.7 (e4m3 11.7 and 9.2), eight 13.0 and 10.9; four experts 4096 -> 1024 9.3 and 12.1.
+    const int64_t weights = std::min<int64_t>(grouped ? p->E : 1, p->rows) * p->N * p->K;
+    const bool streams = weights <= (8 << 20) || (weights <= (16 << 20) && p->rows <= 16 && p->out_dtype != MONDE_E4M3);
+    if (p->rows <= kMatvecRows && streams) return launch_matvec_fp8(P, w, s);
     // Rows picked by id: TMA's gather brings four rows in some 90 cycles, whatever their length, which passes unnoticed behind
     // the weights of a small tile but not at 128 rows (1.5 us per K block, twice the multiplication).  From 32 rows per expert
     // on the rows are first copied side by side into the workspace, behind the space for parts of tiles or, where the workspace
-    // ends before, in its place (tiles are not split then), if there are more tiles than SMs and the copy fits.  128 experts 1024 -> 4096, gathered and copied: 16 rows each 96 and
-    // 100 us, 32 rows 99 and 102, 64 rows 126 and 116, 128 rows 185 and 134; 32 rows on average with a skewed router
-    // (2048 -> 8192) 450 and 404.
+    // ends before, in its place (tiles are not split then), if there are more tiles than SMs and the copy fits.  128 experts
+    // 1024 -> 4096, gathered and copied: 16 rows each 95 and 100 us, 32 rows 110 and 113, 64 rows 128 and 124 (to e4m3 124 and
+    // 114), 128 rows 200 and 147; 32 rows on average with a skewed router (2048 -> 8192) 434 and 388.
     const size_t copy_bytes = static_cast<size_t>(p->rows) * p->K;
     const bool copy_rows = row_ids != nullptr && p->rows >= kCopyRowsPerExpert * p->E &&
                            p->rows / 128 * col_tiles > kMaxSplitUnits / 2 && copy_bytes <= ws_bytes - WsLayout::kHidden;
